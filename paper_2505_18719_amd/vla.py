@@ -2,7 +2,8 @@
 
 Every step of the rollout path runs in the HIP library; this module only
 passes device pointers of torch tensors, the current HIP stream and host
-arrays through the C ABI of ``include/vla.h``.  Importing it fails loudly if
+arrays through the C ABI of ``include/vla.h``, ``include/vla_learn.h`` and
+``include/vla_cache.h``.  Importing it fails loudly if
 the library has not been built.
 """
 from __future__ import annotations
@@ -25,7 +26,9 @@ FLAG_BAD_ACTION = 2
 EXPORTS = ("vla_workspace_size", "vla_create", "vla_prefill", "vla_decode_actions", "vla_token_logprobs",
            "vla_value", "vla_lora_merge", "vla_lora_merge_layer", "vla_read_device_flags", "vla_profile_begin", "vla_profile_end", "vla_destroy",
            "vla_last_error", "vla_extract_actions", "vla_gae", "vla_ppo_clip", "vla_logprob_backward",
-           "vla_train_workspace_size", "vla_ppo_lora_grads")
+           "vla_train_workspace_size", "vla_ppo_lora_grads", "vla_kv_plan", "vla_rope_freqs", "vla_qk_norm_rope",
+           "vla_qk_norm_rope_workspace_size", "vla_qk_norm_rope_backward", "vla_paged_attention_workspace_size",
+           "vla_paged_attention")
 # projections a LoRA adapter merges into (VLA_PROJ_* order), by weight-dict key
 PROJECTIONS = ("wq", "wk", "wv", "wo", "wgate", "wup", "wdown")
 PROF_CATEGORIES = ("prefill_gemm", "prefill_attn", "decode_gemm", "decode_attn", "decode_layer")
@@ -91,6 +94,17 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vla_gae.argtypes = [i32, i32, vp, vp, vp, f32, f32, vp, vp, vp]
     lib.vla_ppo_clip.argtypes = [i32, i32, vp, vp, vp, f32, vp, vp, vp]
     lib.vla_logprob_backward.argtypes = [i32, i32, i32, vp, vp, f32, vp, vp, vp]
+    i64, f64, size = ctypes.c_int64, ctypes.c_double, ctypes.c_size_t
+    lib.vla_kv_plan.argtypes = [i32, vp, vp, vp, i64, i32, vp, i32, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp]
+    lib.vla_rope_freqs.argtypes = [i32, f64, i32, f64, f64, f64, f64, vp, ctypes.POINTER(f32)]
+    lib.vla_qk_norm_rope.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp, vp, i32, i32,
+                                     f32, vp, i64, vp, i64, vp, vp, i32, vp, vp]
+    lib.vla_qk_norm_rope_workspace_size.argtypes = [i32, ctypes.POINTER(size)]
+    lib.vla_qk_norm_rope_backward.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp, f32, vp,
+                                              vp, i32, i32, f32, vp, i64, vp, i64, vp, vp, vp, size, vp]
+    lib.vla_paged_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(size)]
+    lib.vla_paged_attention.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp, f32, vp, i64, vp,
+                                        vp, size, vp]
     lib.vla_profile_begin.argtypes = [vp, ctypes.c_uint32]
     lib.vla_profile_end.argtypes = [vp, vp, vp, vp]
     lib.vla_destroy.argtypes = [vp]
@@ -481,3 +495,224 @@ def logprob_backward(logits: torch.Tensor, tokens: torch.Tensor, action_begin: i
     _check(lib.vla_logprob_backward(rows, bins, int(action_begin), _ptr(logits), _ptr(tokens), float(temperature),
                                     _ptr(dlogp), _ptr(dlogits), _stream(logits.device)))
     return dlogits
+
+
+# ---------------------------------------------------------------- paged cache (vla_cache.h)
+CACHE_PAGE = 16
+CACHE_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+ROPE_SCALINGS = ("none", "linear", "base", "bands", "ramp")
+
+
+class _on:
+    """Makes `device` current for a launch on its stream, where it is not."""
+
+    __slots__ = ("guard",)
+
+    def __init__(self, device):
+        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+    def __enter__(self):
+        if self.guard is not None:
+            self.guard.__enter__()
+
+    def __exit__(self, *exc):
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _at(t: Optional[torch.Tensor], dtype, device, name: str, shape=None):
+    """Address of a contiguous tensor of `dtype` on `device` (None stays None)."""
+    if t is None:
+        return None
+    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and t.shape != shape):
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}"
+                         + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    return t.data_ptr() or None
+
+
+def _head_rows(t: torch.Tensor, like: torch.Tensor, name: str, heads: Optional[int] = None):
+    """Address and row stride of [rows, heads, head_dim] whose rows hold their heads contiguously."""
+    if t.dim() != 3 or t.dtype != like.dtype or t.device != like.device or t.shape[0] != like.shape[0] \
+            or t.shape[2] != like.shape[2] or (heads is not None and t.shape[1] != heads):
+        raise ValueError(f"{name} must be [rows, heads, head_dim] with the rows, head_dim, type and device of q")
+    n, h, d = t.shape
+    sr, sh, sd = t.stride()
+    if sd != 1 or (h > 1 and sh != d):
+        raise ValueError(f"{name} must hold the heads of a row contiguously")
+    return t.data_ptr() or None, (sr if n > 1 else h * d)
+
+
+def _cache_dtype(t: torch.Tensor) -> int:
+    if not t.is_cuda or t.dtype not in CACHE_DTYPES:
+        raise ValueError("expected bfloat16 or float16 device tensors")
+    return CACHE_DTYPES[t.dtype]
+
+
+def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, like: torch.Tensor, kv_heads: Optional[int] = None):
+    """Addresses of the pools, their number of pages and key heads."""
+    n, h, d = k_pages.shape[0], k_pages.shape[1], like.shape[2]
+    if k_pages.dim() != 4 or kv_heads not in (None, h):
+        raise ValueError("k_pages must be [n_pages, n_kv_heads, 16, head_dim]")
+    return (_at(k_pages, like.dtype, like.device, "k_pages", (n, h, CACHE_PAGE, d)),
+            _at(v_pages, like.dtype, like.device, "v_pages", (n, h, d, CACHE_PAGE)), n, h)
+
+
+def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
+               high: float = 4.0, context: float = 8192, device="cuda"):
+    """(freqs fp64 [rot_dim / 2] on `device`, rope_scale) of a rotation (vla_rope_freqs)."""
+    lib = load_library()
+    f = torch.empty(max(0, rot_dim // 2), dtype=torch.float64)
+    scale = ctypes.c_float()
+    _check(lib.vla_rope_freqs(rot_dim, float(base), ROPE_SCALINGS.index(scaling), float(factor), float(low),
+                              float(high), float(context), f.data_ptr(), ctypes.byref(scale)))
+    return f.to(device), scale.value
+
+
+def kv_plan(cached_lens: torch.Tensor, new_lens: torch.Tensor, page_table: torch.Tensor, free_pages: torch.Tensor,
+            n_pages: int, max_rows: int, free_head: Optional[torch.Tensor] = None,
+            out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
+    """New pages (into page_table) and the new tokens' rows of a step (vla_kv_plan): {lens [n_env], row_start [n_env + 1],
+    row_pos, row_env, row_slot [max_rows], stats [3]: free_head after, rows, refused}, all int32."""
+    lib = load_library()
+    dev, i32 = cached_lens.device, torch.int32
+    if not cached_lens.is_cuda or cached_lens.dim() != 1 or page_table.dim() != 2 or free_pages.dim() != 1:
+        raise ValueError("cached_lens [n_env], page_table [n_env, max_pages] and free_pages [n_free] must be device tensors")
+    n, (rows_t, max_pages) = cached_lens.shape[0], page_table.shape
+    if page_table.dtype != i32 or page_table.device != dev or rows_t != n \
+            or (n > 0 and max_pages > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be int32 [n_env, max_pages] with contiguous rows")
+    if out is None:
+        buf = torch.empty(2 * n + 1 + 3 * max_rows + 3, dtype=i32, device=dev)
+        parts = buf.split([n, n + 1, max_rows, max_rows, max_rows, 3])
+        out = dict(zip(("lens", "row_start", "row_pos", "row_env", "row_slot", "stats"), parts))
+    ld = page_table.stride(0) if n > 1 else max_pages
+    with _on(dev):
+        _check(lib.vla_kv_plan(
+            n, _at(cached_lens, i32, dev, "cached_lens"), _at(new_lens, i32, dev, "new_lens", (n,)),
+            page_table.data_ptr() or None, ld, max_pages, _at(free_pages, i32, dev, "free_pages"), free_pages.shape[0],
+            _at(free_head, i32, dev, "free_head", (1,)), n_pages, max_rows, _at(out["lens"], i32, dev, "lens", (n,)),
+            _at(out["row_start"], i32, dev, "row_start", (n + 1,)), _at(out["row_pos"], i32, dev, "row_pos", (max_rows,)),
+            _at(out["row_env"], i32, dev, "row_env", (max_rows,)), _at(out["row_slot"], i32, dev, "row_slot", (max_rows,)),
+            _at(out["stats"], i32, dev, "stats", (3,)), torch.cuda.current_stream(dev).cuda_stream))
+    return out
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, row_pos: Optional[torch.Tensor], freqs: Optional[torch.Tensor],
+                 q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None, eps: float = 1e-6,
+                 layout: str = "half", rope_scale: float = 1.0, v: Optional[torch.Tensor] = None,
+                 k_pages: Optional[torch.Tensor] = None, v_pages: Optional[torch.Tensor] = None,
+                 row_slot: Optional[torch.Tensor] = None, q_out: Optional[torch.Tensor] = None,
+                 k_out: Optional[torch.Tensor] = None):
+    """Head norms and rotation of q [rows, n_heads, head_dim] and k [rows, n_kv_heads, head_dim] (views of one projection's
+    output will do), and with pages the append of k and v at row_slot (vla_qk_norm_rope).  Returns (q_out, k_out); with a
+    cache k_out is written only if it is passed in."""
+    lib = load_library()
+    dt, dev = _cache_dtype(q), q.device
+    rows, H, hd = q.shape
+    K = k.shape[1]
+    cache = k_pages is not None
+    if q_out is None:
+        q_out = torch.empty((rows, H, hd), dtype=q.dtype, device=dev)
+    if k_out is None and not cache:
+        k_out = torch.empty((rows, K, hd), dtype=q.dtype, device=dev)
+    rot = 0 if freqs is None else 2 * freqs.numel()
+    qp, qs = _head_rows(q, q, "q")
+    kp, ks = _head_rows(k, q, "k", K)
+    vp, vs = (None, 0) if v is None else _head_rows(v, q, "v", K)
+    qo, qos = _head_rows(q_out, q, "q_out", H)
+    ko, kos = (None, 0) if k_out is None else _head_rows(k_out, q, "k_out", K)
+    pk, pv, n_pages = _pages(k_pages, v_pages, q, K)[:3] if cache else (None, None, 0)
+    if rows == 0:
+        return q_out, k_out
+    with _on(dev):
+        _check(lib.vla_qk_norm_rope(
+            rows, H, K, hd, dt, qp, qs, kp, ks, vp, vs, _at(q_gain, q.dtype, dev, "q_gain", (hd,)),
+            _at(k_gain, q.dtype, dev, "k_gain", (hd,)), eps, _at(row_pos, torch.int32, dev, "row_pos", (rows,)),
+            _at(freqs, torch.float64, dev, "freqs"), rot, ROPE_LAYOUTS[layout], rope_scale, qo, qos, ko, kos, pk, pv,
+            n_pages, _at(row_slot, torch.int32, dev, "row_slot", (rows,)), torch.cuda.current_stream(dev).cuda_stream))
+    return q_out, k_out
+
+
+def qk_norm_rope_workspace(q: torch.Tensor) -> torch.Tensor:
+    """The workspace of qk_norm_rope_backward for heads like q's."""
+    lib = load_library()
+    n = ctypes.c_size_t()
+    _check(lib.vla_qk_norm_rope_workspace_size(q.shape[2], ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=q.device)
+
+
+def qk_norm_rope_backward(q: Optional[torch.Tensor], k: Optional[torch.Tensor], dq_out: torch.Tensor,
+                          dk_out: torch.Tensor, row_pos: Optional[torch.Tensor], freqs: Optional[torch.Tensor],
+                          q_gain: Optional[torch.Tensor] = None, k_gain: Optional[torch.Tensor] = None,
+                          eps: float = 1e-6, layout: str = "half", rope_scale: float = 1.0,
+                          dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                          workspace: Optional[torch.Tensor] = None):
+    """(dq, dk, dq_gain, dk_gain) of qk_norm_rope from its inputs and the gradients of its outputs
+    (vla_qk_norm_rope_backward); the gains' gradients are fp32 [head_dim], None without the gain.  q and k may be None where
+    they have no gain."""
+    lib = load_library()
+    dt, dev = _cache_dtype(dq_out), dq_out.device
+    rows, H, hd = dq_out.shape
+    K = dk_out.shape[1]
+    if dq is None:
+        dq = torch.empty((rows, H, hd), dtype=dq_out.dtype, device=dev)
+    if dk is None:
+        dk = torch.empty((rows, K, hd), dtype=dq_out.dtype, device=dev)
+    dq_gain = None if q_gain is None else torch.empty(hd, dtype=torch.float32, device=dev)
+    dk_gain = None if k_gain is None else torch.empty(hd, dtype=torch.float32, device=dev)
+    if workspace is None and (q_gain is not None or k_gain is not None):
+        workspace = qk_norm_rope_workspace(dq_out)
+    rot = 0 if freqs is None else 2 * freqs.numel()
+    qp, qs = (None, 0) if q is None else _head_rows(q, dq_out, "q", H)
+    kp, ks = (None, 0) if k is None else _head_rows(k, dq_out, "k", K)
+    gq, gqs = _head_rows(dq_out, dq_out, "dq_out")
+    gk, gks = _head_rows(dk_out, dq_out, "dk_out", K)
+    oq, oqs = _head_rows(dq, dq_out, "dq", H)
+    ok, oks = _head_rows(dk, dq_out, "dk", K)
+    with _on(dev):
+        _check(lib.vla_qk_norm_rope_backward(
+            rows, H, K, hd, dt, qp, qs, kp, ks, gq, gqs, gk, gks, _at(q_gain, dq_out.dtype, dev, "q_gain", (hd,)),
+            _at(k_gain, dq_out.dtype, dev, "k_gain", (hd,)), eps, _at(row_pos, torch.int32, dev, "row_pos", (rows,)),
+            _at(freqs, torch.float64, dev, "freqs"), rot, ROPE_LAYOUTS[layout], rope_scale, oq, oqs, ok, oks,
+            None if dq_gain is None else dq_gain.data_ptr(), None if dk_gain is None else dk_gain.data_ptr(),
+            _at(workspace, torch.uint8, dev, "workspace"), 0 if workspace is None else workspace.numel(),
+            torch.cuda.current_stream(dev).cuda_stream))
+    return dq, dk, dq_gain, dk_gain
+
+
+def paged_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor) -> torch.Tensor:
+    """The workspace of paged_attention for calls of these shapes."""
+    lib = load_library()
+    n = ctypes.c_size_t()
+    _check(lib.vla_paged_attention_workspace_size(q.shape[0], q.shape[1], k_pages.shape[1], q.shape[2],
+                                                  page_table.shape[1], ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=q.device)
+
+
+def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                    lens: torch.Tensor, scale: float, out: Optional[torch.Tensor] = None,
+                    lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention [n_env, n_heads, head_dim] of one token per environment over its lens[e] cached tokens
+    (vla_paged_attention); lse fp32 [n_env, n_heads], if passed in, receives the log-sum-exp of the scores."""
+    lib = load_library()
+    dt, dev = _cache_dtype(q), q.device
+    n, H, hd = q.shape
+    if out is None:
+        out = torch.empty((n, H, hd), dtype=q.dtype, device=dev)
+    qp, qs = _head_rows(q, q, "q")
+    op, os_ = _head_rows(out, q, "out", H)
+    pk, pv, n_pages, K = _pages(k_pages, v_pages, q)
+    if page_table.dtype != torch.int32 or page_table.device != dev or page_table.dim() != 2 or page_table.shape[0] != n \
+            or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
+        raise ValueError("page_table must be int32 [n_env, max_pages] with contiguous rows")
+    max_pages = page_table.shape[1]
+    if workspace is None:
+        workspace = paged_attention_workspace(q, k_pages, page_table)
+    with _on(dev):
+        _check(lib.vla_paged_attention(
+            n, H, K, hd, dt, qp, qs, pk, pv, n_pages, page_table.data_ptr() or None,
+            page_table.stride(0) if n > 1 else max_pages, max_pages, _at(lens, torch.int32, dev, "lens", (n,)), scale, op,
+            os_, _at(lse, torch.float32, dev, "lse", (n, H)), _at(workspace, torch.uint8, dev, "workspace"),
+            workspace.numel(), torch.cuda.current_stream(dev).cuda_stream))
+    return out
