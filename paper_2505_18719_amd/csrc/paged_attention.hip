@@ -1,5 +1,15 @@
 // Attention of one new token per environment over a paged KV cache of any length (vla_paged_attention).
+//
+// Bound: HBM, every cached key and value once (4 head_dim bytes a key and key head), against 4 flops per byte and query head
+// of a group.  A wave takes steps of 32 keys, two pages, for up to 16 or 32 query heads of one key head, all on 16x16x32
+// MFMAs: S^T = K Q^T with the keys on the rows, placed so that lane group g = lane / 16 ends up with the scores of keys
+// 8 g .. 8 g + 7 of the step for head lane % 16, which is the B operand of O^T += V^T P^T as it stands; the transposed value
+// pages give the A operand by one 16-byte load per lane.  Nothing goes through LDS but the joins.  Softmax by a running
+// maximum and sum per head in fp32 (base 2); the weights enter the second product as a pair of numbers of the cache's type
+// (hi + lo, 16 bits or more), so that their rounding stays below the output's.
 #include <hip/hip_runtime.h>
+
+#include <algorithm>
 
 #include "cache.h"
 #include "common.h"
@@ -7,90 +17,468 @@
 namespace vla {
 namespace {
 
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+
+constexpr int kStep = 32;  // keys of a wave's step
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
 template <CacheType T>
-__device__ __forceinline__ float to_f32(bf16_t h) {
-  if constexpr (T == kBf16) return bf2f(h);
-  else return (float)__builtin_bit_cast(_Float16, h);
+__device__ __forceinline__ f32x4 mfma(const uint4& a, const uint4& b, const f32x4& c) {
+  if constexpr (T == kBf16) return mfma16(as_bf16x8(a), as_bf16x8(b), c);
+  else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+
 template <CacheType T>
 __device__ __forceinline__ bf16_t from_f32(float f) {
   if constexpr (T == kBf16) return f2bf(f);
   else return __builtin_bit_cast(bf16_t, (_Float16)f);
 }
 
-constexpr int kAttnThreads = 256, kAttnWaves = kAttnThreads / kWave;
-
-// One workgroup per (environment, head); wave w takes keys w, w + 4, ... with a running maximum and sum, a lane holding
-// features lane, lane + 64, ...; the waves are joined in LDS.
-template <int HD, CacheType T>
-__global__ __launch_bounds__(kAttnThreads) void paged_attn_kernel(PagedAttnArgs a) {
-  constexpr int N = HD / kWave;
-  __shared__ float ms[kAttnWaves], ls[kAttnWaves], os[kAttnWaves][HD];
-  const int head = blockIdx.x, env = blockIdx.y, lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-  const int kvh = head / (a.n_heads / a.n_kv_heads);
-  const long long len = a.lens[env];
-  const bool bad = len < 0 || len > (long long)a.max_pages * kPage;
-  const int32_t* pt = a.page_table + env * a.ld_table;
-  float q[N], o[N], m = -INFINITY, l = bad ? __builtin_nanf("") : 0.f;
+// hi + lo = p[0 .. 8) to the precision of two numbers of the type
+template <CacheType T>
+__device__ __forceinline__ void split_weights(const float* p, uint4& hi, uint4& lo) {
+  if constexpr (T == kBf16) {
+    uint32_t h[4], r[4];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    q[i] = to_f32<T>(a.q[env * a.ld_q + head * HD + lane + 64 * i]);
-    o[i] = 0.f;
-  }
-  for (long long key = w; !bad && key < len; key += kAttnWaves) {
-    const int page = pt[key / kPage], slot = (int)(key % kPage);
-    if (page < 0 || page >= a.n_pages) {
-      l = __builtin_nanf("");
-      break;
+    for (int i = 0; i < 4; ++i) {
+      h[i] = pack2bf(p[2 * i], p[2 * i + 1]);
+      r[i] = pack2bf(p[2 * i] - __uint_as_float(h[i] << 16), p[2 * i + 1] - __uint_as_float(h[i] & 0xffff0000u));
     }
-    const size_t at = (size_t)page * a.n_kv_heads + kvh;
-    float s = 0.f;
+    hi = make_uint4(h[0], h[1], h[2], h[3]);
+    lo = make_uint4(r[0], r[1], r[2], r[3]);
+  } else {
+    f16x8 h, r;
 #pragma unroll
-    for (int i = 0; i < N; ++i) s += q[i] * to_f32<T>(a.pages.k[(at * kPage + slot) * HD + lane + 64 * i]);
-    s = wave_sum(s) * a.scale;
-    const float mn = fmaxf(m, s), c = m == -INFINITY ? 0.f : expf(m - mn), p = mn == -INFINITY ? 0.f : expf(s - mn);
-    l = l * c + p;
-#pragma unroll
-    for (int i = 0; i < N; ++i) o[i] = o[i] * c + p * to_f32<T>(a.pages.v[(at * HD + lane + 64 * i) * kPage + slot]);
-    m = mn;
+    for (int i = 0; i < 8; ++i) {
+      h[i] = (_Float16)p[i];
+      r[i] = (_Float16)(p[i] - (float)h[i]);
+    }
+    hi = __builtin_bit_cast(uint4, h);
+    lo = __builtin_bit_cast(uint4, r);
   }
-  if (lane == 0) {
-    ms[w] = m;
-    ls[w] = l;
-  }
-#pragma unroll
-  for (int i = 0; i < N; ++i) os[w][lane + 64 * i] = o[i];
-  __syncthreads();
-  float mm = -INFINITY, ll = 0.f;
-#pragma unroll
-  for (int u = 0; u < kAttnWaves; ++u) mm = fmaxf(mm, ms[u]);
-#pragma unroll
-  for (int u = 0; u < kAttnWaves; ++u) ll += ls[u] * (ms[u] == -INFINITY ? 0.f : expf(ms[u] - mm));
-  for (int f = threadIdx.x; f < HD; f += kAttnThreads) {
-    float v = 0.f;
-#pragma unroll
-    for (int u = 0; u < kAttnWaves; ++u) v += os[u][f] * (ms[u] == -INFINITY ? 0.f : expf(ms[u] - mm));
-    a.o[env * a.ld_o + head * HD + f] = from_f32<T>(ll == 0.f ? 0.f : v / ll);
-  }
-  if (a.lse && threadIdx.x == 0) a.lse[(size_t)env * a.n_heads + head] = mm + logf(ll);
+}
+// Half-precision weights are held 2^15 times as large: the largest stays below 65504, and a weight is lost only below 2^-40
+// of it, where even 2^18 such keys do not show.
+template <CacheType T>
+constexpr float kWeightExp = T == kBf16 ? 0.f : 15.f;
+
+// Max / sum over the lanes that share lane % 16.
+__device__ __forceinline__ float column_max(float v) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float column_sum(float v) {
+  auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
 
-template <CacheType T>
-hipError_t launch_t(const PagedAttnArgs& a, hipStream_t s) {
-  const dim3 grid(a.n_heads, a.n_env), block(kAttnThreads);
-  if (a.head_dim == 64) hipLaunchKernelGGL((paged_attn_kernel<64, T>), grid, block, 0, s, a);
-  else if (a.head_dim == 128) hipLaunchKernelGGL((paged_attn_kernel<128, T>), grid, block, 0, s, a);
-  else if (a.head_dim == 256) hipLaunchKernelGGL((paged_attn_kernel<256, T>), grid, block, 0, s, a);
-  else return hipErrorInvalidValue;
+// One block of up to 16 QT query heads of a key head.
+struct HeadBlock {
+  int kvh, head0, n;  // key head, first query head, query heads
+};
+template <int QT>
+__host__ __device__ __forceinline__ int head_blocks(int group) { return (group + 16 * QT - 1) / (16 * QT); }
+template <int QT>
+__device__ __forceinline__ HeadBlock head_block(const PagedAttnArgs& a, int hb) {
+  const int group = a.n_heads / a.n_kv_heads, qb = head_blocks<QT>(group);
+  const int kvh = hb / qb, first = hb % qb * 16 * QT;
+  return {kvh, kvh * group + first, min(group - first, 16 * QT)};
+}
+
+// What a wave holds of its keys: per head (lane % 16, tile t) the running maximum m of the base-2 scores, this lane's part
+// of the sum l of weights, and O^T: features 16 i + 4 (lane / 16) + r in o[t][i][r].
+template <int HD, int QT>
+struct Running {
+  float m[QT], l[QT];
+  f32x4 o[QT][HD / 16];
+};
+
+// Steps s0, s0 + stride, ... below s1 of environment `env`, of `len` keys, for head block b.
+template <int HD, CacheType T, int QT>
+__device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const HeadBlock& b, int len, int s0, int s1, int stride,
+                                       Running<HD, QT>& run) {
+  constexpr int KC = HD / 32, VC = HD / 16;
+  const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
+  const float scale = a.scale * kLog2e;
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    run.m[t] = -INFINITY;
+    run.l[t] = 0.f;
+#pragma unroll
+    for (int i = 0; i < VC; ++i) run.o[t][i] = {0.f, 0.f, 0.f, 0.f};
+  }
+  if (s0 >= s1) return;
+  uint4 q[QT][KC];
+#pragma unroll
+  for (int t = 0; t < QT; ++t)
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+      q[t][i] = make_uint4(0, 0, 0, 0);
+      if (16 * t + m16 < b.n)
+        q[t][i] = *reinterpret_cast<const uint4*>(a.q + env * a.ld_q + (size_t)(b.head0 + 16 * t + m16) * HD + 32 * i + 8 * g);
+    }
+  const int32_t* pt = a.page_table + env * a.ld_table;
+  const int last = (len - 1) / kPage;
+  const size_t page_elems = (size_t)a.n_kv_heads * kPage * HD;
+  // row lane % 16 of the K operand of tile t: page m16 / 8 of the step, slot 8 (m16 / 4 % 2) + 4 t + m16 % 4
+  const bf16_t* kb = a.pages.k + ((size_t)b.kvh * kPage + 8 * ((m16 >> 2) & 1) + (m16 & 3)) * HD + 8 * g;
+  const bf16_t* vb = a.pages.v + ((size_t)b.kvh * HD + m16) * kPage + 8 * (g & 1);
+  for (int s = s0; s < s1; s += stride) {
+    int p0 = pt[2 * s], p1 = pt[min(2 * s + 1, last)];
+    if ((unsigned)p0 >= (unsigned)a.n_pages || (unsigned)p1 >= (unsigned)a.n_pages) {  // a bad page: NaN from here on
+      p0 = p1 = 0;
+#pragma unroll
+      for (int t = 0; t < QT; ++t) run.l[t] = __builtin_nanf("");
+    }
+    const bf16_t* kp = kb + (m16 < 8 ? p0 : p1) * page_elems;
+    const bf16_t* vp = vb + (g < 2 ? p0 : p1) * page_elems;
+    uint4 k[2][KC], v[VC];
+#pragma unroll
+    for (int i = 0; i < KC; ++i)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) k[t][i] = *reinterpret_cast<const uint4*>(kp + 4 * t * HD + 32 * i);
+#pragma unroll
+    for (int i = 0; i < VC; ++i) v[i] = *reinterpret_cast<const uint4*>(vp + 16 * i * kPage);
+    const int left = len - kStep * s;  // keys of the step that count
+    if (left < kStep) {  // slots past the length hold anything: 0 weights must multiply finite values
+      uint32_t keep[4];
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        keep[d] = (8 * g + 2 * d < left ? 0xffffu : 0u) | (8 * g + 2 * d + 1 < left ? 0xffff0000u : 0u);
+#pragma unroll
+      for (int i = 0; i < VC; ++i) v[i] = make_uint4(v[i].x & keep[0], v[i].y & keep[1], v[i].z & keep[2], v[i].w & keep[3]);
+    }
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      float p[8];
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        f32x4 c = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < KC; ++i) c = mfma<T>(k[u][i], q[t][i], c);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[4 * u + r] = c[r] * scale;
+      }
+      if (left < kStep) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (8 * g + j >= left) p[j] = -INFINITY;
+      }
+      float mx = p[0];
+#pragma unroll
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, p[j]);
+      mx = fmaxf(run.m[t], column_max(mx));
+      if (__any(mx > run.m[t])) {  // seldom after the first steps
+        const float c = run.m[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run.m[t] - mx);  // nothing to scale yet: 1
+        run.l[t] *= c;
+#pragma unroll
+        for (int i = 0; i < VC; ++i) run.o[t][i] *= c;
+        run.m[t] = mx;
+      }
+      const float base = run.m[t] == -INFINITY ? 0.f : run.m[t] - kWeightExp<T>;
+      float sum = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        p[j] = __builtin_amdgcn_exp2f(p[j] - base);
+        sum += p[j];
+      }
+      run.l[t] += sum;
+      uint4 hi, lo;
+      split_weights<T>(p, hi, lo);
+#pragma unroll
+      for (int i = 0; i < VC; ++i) {
+        run.o[t][i] = mfma<T>(v[i], hi, run.o[t][i]);
+        run.o[t][i] = mfma<T>(v[i], lo, run.o[t][i]);
+      }
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < QT; ++t) run.l[t] = column_sum(run.l[t]);
+}
+
+// Where the joined result of a head block goes: the output, or a partial (o fp32 [16 QT][HD], m and l [16 QT] each).
+struct Partial {
+  float* o;
+  float* ml;
+};
+
+// Joins the W waves' parts, 64 features at a time through LDS, and writes the output rows (part.o == null) or the partial.
+template <int HD, CacheType T, int QT, int W>
+__device__ __forceinline__ void join_waves(const PagedAttnArgs& a, int env, const HeadBlock& b, Running<HD, QT>& run, Partial part) {
+  constexpr int FS = 68;  // row of 64 features, padded
+  __shared__ float sm[W][16 * QT], sl[W][16 * QT];
+  __shared__ __align__(16) float so[W][16 * QT][FS];
+  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m16 = lane & 15, g = lane >> 4;
+  if (g == 0) {
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      sm[w][16 * t + m16] = run.m[t];
+      sl[w][16 * t + m16] = run.l[t];
+    }
+  }
+  __syncthreads();
+  float scale[QT];
+#pragma unroll
+  for (int t = 0; t < QT; ++t) {
+    float m = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < W; ++u) m = fmaxf(m, sm[u][16 * t + m16]);
+    scale[t] = run.m[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run.m[t] - m);
+  }
+#pragma unroll
+  for (int f0 = 0; f0 < HD / 64; ++f0) {
+    if (f0) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+        *reinterpret_cast<f32x4*>(&so[w][16 * t + m16][16 * i + 4 * g]) = run.o[t][4 * f0 + i] * scale[t];
+    __syncthreads();
+    for (int i = tid; i < b.n * 64; i += 64 * W) {
+      const int h = i / 64, f = i % 64;
+      float v = 0.f, m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int u = 0; u < W; ++u) {
+        v += so[u][h][f];
+        m = fmaxf(m, sm[u][h]);
+      }
+#pragma unroll
+      for (int u = 0; u < W; ++u) l += sl[u][h] * (sm[u][h] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[u][h] - m));
+      if (part.o) {
+        part.o[h * HD + 64 * f0 + f] = v;
+        if (f0 == 0 && f == 0) {
+          part.ml[h] = m;
+          part.ml[16 * QT + h] = l;
+        }
+      } else {
+        a.o[env * a.ld_o + (size_t)(b.head0 + h) * HD + 64 * f0 + f] = from_f32<T>(l == 0.f ? 0.f : v / l);
+        if (a.lse && f0 == 0 && f == 0)
+          a.lse[(size_t)env * a.n_heads + b.head0 + h] = (m - kWeightExp<T> + __builtin_amdgcn_logf(l)) * kLn2;
+      }
+    }
+  }
+}
+
+// An environment's number of steps; 0 for one that gets zeros or NaN.
+__device__ __forceinline__ int steps_of(const PagedAttnArgs& a, int len) {
+  const bool bad = len < 0 || len > (long long)a.max_pages * kPage || a.n_pages == 0;
+  return bad ? 0 : (len + kStep - 1) / kStep;
+}
+
+// The rows of a head block of an environment without steps: zeros for length 0, else NaN.
+template <int HD, CacheType T>
+__device__ __forceinline__ void no_keys(const PagedAttnArgs& a, int env, int head0, int n, int len) {
+  const float v = len == 0 ? 0.f : __builtin_nanf("");
+  for (int i = threadIdx.x; i < n * HD; i += blockDim.x) a.o[env * a.ld_o + (size_t)head0 * HD + i] = from_f32<T>(v);
+  if (a.lse && (int)threadIdx.x < n) a.lse[(size_t)env * a.n_heads + head0 + threadIdx.x] = len == 0 ? -INFINITY : v;
+}
+
+// One workgroup of W waves per (head block, environment).
+template <int HD, CacheType T, int QT, int W>
+__global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a) {
+  const int env = blockIdx.y, len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
+  const HeadBlock b = head_block<QT>(a, blockIdx.x);
+  if (steps == 0) return no_keys<HD, T>(a, env, b.head0, b.n, len);
+  Running<HD, QT> run;
+  attend<HD, T, QT>(a, env, b, len, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), steps, W, run);
+  join_waves<HD, T, QT, W>(a, env, b, run, {nullptr, nullptr});
+}
+
+// ------------------------------------------------------------------ split over the keys
+// The steps of all environments and head blocks lie in one line, environment by environment, head block by head block; a
+// persistent grid of workgroups takes equal runs of it.  A workgroup's first and last run of one (environment, head block)
+// may be a part of it: then it leaves a partial, in slot 2 w where an earlier workgroup began the line's piece, else in 2 w
+// + 1, and attn_join_kernel joins a piece's partials in order.  The line's start of every environment goes to the workspace.
+constexpr int kSplitGroups = 512, kSplitWaves = 4;
+constexpr int kSplitMinSteps = kSplitWaves;  // steps per workgroup at least
+
+__host__ __device__ __forceinline__ int split_workers(long long units) {
+  const long long w = (units + kSplitMinSteps - 1) / kSplitMinSteps;
+  return w < kSplitGroups ? (int)w : kSplitGroups;
+}
+__device__ __forceinline__ long long worker_start(long long units, int workers, int w) { return units * w / workers; }
+// worker whose run holds unit u
+__device__ __forceinline__ int worker_of(long long units, int workers, long long u) {
+  return (int)(((u + 1) * workers + units - 1) / units) - 1;
+}
+
+struct SplitSpace {
+  long long* start;  // [n_env + 1] first unit of each environment
+  float* o;          // [2 kSplitGroups][16 QT][HD]
+  float* ml;         // [2 kSplitGroups][2][16 QT]
+};
+size_t space_start_bytes(int n_env) { return ((size_t)(n_env + 1) * 8 + 255) / 256 * 256; }
+template <int HD, int QT>
+SplitSpace split_space(void* ws, int n_env) {
+  char* p = static_cast<char*>(ws);
+  float* o = reinterpret_cast<float*>(p + space_start_bytes(n_env));
+  return {reinterpret_cast<long long*>(p), o, o + (size_t)2 * kSplitGroups * 16 * QT * HD};
+}
+
+template <int HD, CacheType T, int QT>
+__global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnArgs a, SplitSpace sp, int blocks) {
+  constexpr int NT = 64 * kSplitWaves;
+  __shared__ long long sums[NT];
+  __shared__ long long found_base;
+  __shared__ int found_env;
+  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), me = blockIdx.x;
+  // every workgroup adds up the steps of all environments: thread t those of a run of them
+  const int per = (a.n_env + NT - 1) / NT, e0 = min(a.n_env, tid * per), e1 = min(a.n_env, e0 + per);
+  long long mine = 0;
+  for (int e = e0; e < e1; ++e) mine += steps_of(a, a.lens[e]);
+  sums[tid] = mine;
+  __syncthreads();
+  for (int o = 1; o < NT; o <<= 1) {
+    const long long v = tid >= o ? sums[tid - o] : 0;
+    __syncthreads();
+    sums[tid] += v;
+    __syncthreads();
+  }
+  const long long units = sums[NT - 1] * blocks;
+  if (me == 0) {
+    long long at = (sums[tid] - mine) * blocks;
+    for (int e = e0; e < e1; ++e) {
+      sp.start[e] = at;
+      at += (long long)steps_of(a, a.lens[e]) * blocks;
+    }
+    if (tid == NT - 1) sp.start[a.n_env] = units;
+  }
+  const int workers = split_workers(units);
+  if (me >= workers) return;
+  long long u = worker_start(units, workers, me);
+  const long long u1 = worker_start(units, workers, me + 1), begin = u;
+  if (mine > 0 && (sums[tid] - mine) * blocks <= u && u < sums[tid] * blocks) {
+    long long at = (sums[tid] - mine) * blocks;
+    int e = e0;
+    for (;; ++e) {
+      const long long n = (long long)steps_of(a, a.lens[e]) * blocks;
+      if (u < at + n) break;
+      at += n;
+    }
+    found_base = at;
+    found_env = e;
+  }
+  __syncthreads();
+  long long base = found_base;
+  int env = __builtin_amdgcn_readfirstlane(found_env);
+  while (u < u1) {
+    const int len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
+    if (steps > 0) {
+      while (u < u1 && u < base + (long long)steps * blocks) {
+        const int hb = __builtin_amdgcn_readfirstlane((int)((u - base) / steps)), s0 = __builtin_amdgcn_readfirstlane((int)((u - base) % steps));
+        const int n = __builtin_amdgcn_readfirstlane((int)min((long long)(steps - s0), u1 - u));
+        const HeadBlock b = head_block<QT>(a, hb);
+        Running<HD, QT> run;
+        attend<HD, T, QT>(a, env, b, len, s0 + w, s0 + n, kSplitWaves, run);
+        Partial part = {nullptr, nullptr};
+        if (n < steps) {
+          const size_t slot = 2 * (size_t)me + (u - s0 < begin ? 0 : 1);
+          part = {sp.o + slot * 16 * QT * HD, sp.ml + slot * 2 * 16 * QT};
+        }
+        __syncthreads();  // the last join's reads of LDS
+        join_waves<HD, T, QT, kSplitWaves>(a, env, b, run, part);
+        u += n;
+      }
+      base += (long long)steps * blocks;
+    }
+    ++env;
+  }
+}
+
+// One workgroup per (query head, environment): joins the partials of its head's keys, or writes the row of an environment
+// without steps; a piece that one workgroup held whole is done.
+constexpr int kJoinThreads = 512;
+template <int HD, CacheType T, int QT>
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp, int blocks) {
+  constexpr int PG = kJoinThreads / HD;  // runs of partials added side by side
+  __shared__ float so[PG][HD], sl[PG];
+  __shared__ float sm[kJoinThreads / kWave];
+  const int head = blockIdx.x, env = blockIdx.y, tid = threadIdx.x;
+  const int len = a.lens[env], steps = steps_of(a, len);
+  if (steps == 0) return no_keys<HD, T>(a, env, head, 1, len);
+  const long long units = sp.start[a.n_env];
+  const int group = a.n_heads / a.n_kv_heads, hb = head / group * head_blocks<QT>(group) + head % group / (16 * QT);
+  const int row = head % group % (16 * QT), workers = split_workers(units);
+  const long long u0 = sp.start[env] + (long long)hb * steps, u1 = u0 + steps;
+  const int w0 = worker_of(units, workers, u0), w1 = worker_of(units, workers, u1 - 1);
+  if (w0 == w1) return;
+  // worker w0 began the piece; the others went on with it
+  auto slot = [&](int w) { return 2 * (size_t)w + (w == w0 ? 1 : 0); };
+  float m = -INFINITY;
+  for (int w = w0 + tid; w <= w1; w += kJoinThreads) m = fmaxf(m, sp.ml[slot(w) * 2 * 16 * QT + row]);
+  m = wave_max(m);
+  if ((tid & 63) == 0) sm[tid >> 6] = m;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kJoinThreads / kWave; ++i) m = fmaxf(m, sm[i]);
+  const int f = tid % HD, pg = tid / HD;
+  float v = 0.f, l = 0.f;
+  for (int w = w0 + pg; w <= w1; w += PG) {
+    const float* ml = sp.ml + slot(w) * 2 * 16 * QT;
+    const float c = ml[row] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[row] - m);
+    v = fmaf(sp.o[slot(w) * 16 * QT * HD + row * HD + f], c, v);
+    l = fmaf(ml[16 * QT + row], c, l);
+  }
+  so[pg][f] = v;
+  if (f == 0) sl[pg] = l;
+  __syncthreads();
+  if (pg > 0) return;
+  v = l = 0.f;
+#pragma unroll
+  for (int i = 0; i < PG; ++i) {
+    v += so[i][f];
+    l += sl[i];
+  }
+  a.o[env * a.ld_o + (size_t)head * HD + f] = from_f32<T>(l == 0.f ? 0.f : v / l);
+  if (a.lse && f == 0) a.lse[(size_t)env * a.n_heads + head] = (m - kWeightExp<T> + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+// ------------------------------------------------------------------ host
+bool split_keys(int max_pages) { return max_pages > 32; }
+
+template <int HD, CacheType T, int QT>
+hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
+  const int blocks = head_blocks<QT>(a.n_heads / a.n_kv_heads) * a.n_kv_heads;
+  const dim3 grid(blocks, a.n_env);
+  if (!split_keys(a.max_pages)) {
+    hipLaunchKernelGGL((attn_whole_kernel<HD, T, QT, 4>), grid, dim3(256), 0, s, a);
+  } else {
+    const SplitSpace sp = split_space<HD, QT>(a.ws, a.n_env);
+    hipLaunchKernelGGL((attn_split_kernel<HD, T, QT>), dim3(kSplitGroups), dim3(64 * kSplitWaves), 0, s, a, sp, blocks);
+    hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(a.n_heads, a.n_env), dim3(kJoinThreads), 0, s, a, sp, blocks);
+  }
   return hipGetLastError();
+}
+
+// Query heads of a group by tiles of 16: two share a step's keys in registers, more read them again.
+int query_tiles(int n_heads, int n_kv_heads) { return n_heads / n_kv_heads > 16 ? 2 : 1; }
+
+template <int HD, CacheType T>
+hipError_t launch_heads(const PagedAttnArgs& a, hipStream_t s) {
+  return query_tiles(a.n_heads, a.n_kv_heads) == 1 ? launch_blocks<HD, T, 1>(a, s) : launch_blocks<HD, T, 2>(a, s);
+}
+template <CacheType T>
+hipError_t launch_type(const PagedAttnArgs& a, hipStream_t s) {
+  if (a.head_dim == 64) return launch_heads<64, T>(a, s);
+  if (a.head_dim == 128) return launch_heads<128, T>(a, s);
+  if (a.head_dim == 256) return launch_heads<256, T>(a, s);
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-size_t paged_attn_bytes(int, int, int, int, int) { return 256; }
+size_t paged_attn_bytes(int n_env, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
+  if (!split_keys(max_pages)) return 256;
+  const size_t rows = 16 * query_tiles(n_heads, n_kv_heads);
+  return space_start_bytes(n_env) + (size_t)2 * kSplitGroups * rows * (head_dim + 2) * sizeof(float);
+}
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
-  return a.type == kBf16 ? launch_t<kBf16>(a, s) : launch_t<kF16>(a, s);
+  return a.type == kBf16 ? launch_type<kBf16>(a, s) : launch_type<kF16>(a, s);
 }
 
 }  // namespace vla
