@@ -97,10 +97,23 @@ struct Running {
   f32x4 o[QT][HD / 16];
 };
 
-// Steps s0, s0 + stride, ... below s1 of environment `env`, of `len` keys, for head block b.
+typedef unsigned u32x4v __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ uint4 load_once(const bf16_t* p) {  // past the caches: a page is read by one wave
+  const u32x4v v = __builtin_nontemporal_load(reinterpret_cast<const u32x4v*>(p));
+  return make_uint4(v.x, v.y, v.z, v.w);
+}
+
+// The pages of step s; entries up to the table's end may be read before the length is known.
+__device__ __forceinline__ int2 step_pages(const PagedAttnArgs& a, const int32_t* pt, int s) {
+  return make_int2(pt[min(2 * s, a.max_pages - 1)], pt[min(2 * s + 1, a.max_pages - 1)]);
+}
+
+// Steps s0, s0 + stride, ... below s1 of environment `env`, of `len` keys, for head block b; `ids` are step s0's pages.  A
+// step's keys are requested as soon as the step before has used its own, its values likewise, so that a wave always has one
+// step's pages on the way.
 template <int HD, CacheType T, int QT>
 __device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const HeadBlock& b, int len, int s0, int s1, int stride,
-                                       Running<HD, QT>& run) {
+                                       int2 ids, Running<HD, QT>& run) {
   constexpr int KC = HD / 32, VC = HD / 16;
   const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
   const float scale = a.scale * kLog2e;
@@ -127,50 +140,63 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const He
   // row lane % 16 of the K operand of tile t: page m16 / 8 of the step, slot 8 (m16 / 4 % 2) + 4 t + m16 % 4
   const bf16_t* kb = a.pages.k + ((size_t)b.kvh * kPage + 8 * ((m16 >> 2) & 1) + (m16 & 3)) * HD + 8 * g;
   const bf16_t* vb = a.pages.v + ((size_t)b.kvh * HD + m16) * kPage + 8 * (g & 1);
-  for (int s = s0; s < s1; s += stride) {
-    int p0 = pt[2 * s], p1 = pt[min(2 * s + 1, last)];
-    if ((unsigned)p0 >= (unsigned)a.n_pages || (unsigned)p1 >= (unsigned)a.n_pages) {  // a bad page: NaN from here on
-      p0 = p1 = 0;
-#pragma unroll
-      for (int t = 0; t < QT; ++t) run.l[t] = __builtin_nanf("");
+  bool bad = false;
+  auto check = [&](int s) {  // a bad page is not read: NaN from there on
+    if (2 * s + 1 > last) ids.y = ids.x;
+    if ((unsigned)ids.x >= (unsigned)a.n_pages || (unsigned)ids.y >= (unsigned)a.n_pages) {
+      ids = make_int2(0, 0);
+      bad = true;
     }
-    const bf16_t* kp = kb + (m16 < 8 ? p0 : p1) * page_elems;
-    const bf16_t* vp = vb + (g < 2 ? p0 : p1) * page_elems;
-    uint4 k[2][KC], v[VC];
+  };
+  uint4 k[2][KC], v[VC];
+  auto load_k = [&] {
+    const bf16_t* kp = kb + (m16 < 8 ? ids.x : ids.y) * page_elems;
 #pragma unroll
     for (int i = 0; i < KC; ++i)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) k[t][i] = *reinterpret_cast<const uint4*>(kp + 4 * t * HD + 32 * i);
+      for (int t = 0; t < 2; ++t) k[t][i] = load_once(kp + 4 * t * HD + 32 * i);
+  };
+  auto load_v = [&](const bf16_t* vp) {
 #pragma unroll
-    for (int i = 0; i < VC; ++i) v[i] = *reinterpret_cast<const uint4*>(vp + 16 * i * kPage);
+    for (int i = 0; i < VC; ++i) v[i] = load_once(vp + 16 * i * kPage);
+  };
+  check(s0);
+  load_k();
+  load_v(vb + (g < 2 ? ids.x : ids.y) * page_elems);
+  int2 after = step_pages(a, pt, s0 + stride);  // of the next step
+  for (int s = s0; s < s1; s += stride) {
     const int left = len - kStep * s;  // keys of the step that count
-    if (left < kStep) {  // slots past the length hold anything: 0 weights must multiply finite values
-      uint32_t keep[4];
+    const bool more = s + stride < s1;
+    float p[QT][8];
 #pragma unroll
-      for (int d = 0; d < 4; ++d)
-        keep[d] = (8 * g + 2 * d < left ? 0xffffu : 0u) | (8 * g + 2 * d + 1 < left ? 0xffff0000u : 0u);
-#pragma unroll
-      for (int i = 0; i < VC; ++i) v[i] = make_uint4(v[i].x & keep[0], v[i].y & keep[1], v[i].z & keep[2], v[i].w & keep[3]);
-    }
-#pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      float p[8];
+    for (int t = 0; t < QT; ++t)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         f32x4 c = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < KC; ++i) c = mfma<T>(k[u][i], q[t][i], c);
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[4 * u + r] = c[r] * scale;
+        for (int r = 0; r < 4; ++r) p[t][4 * u + r] = c[r] * scale;
       }
+    const bf16_t* next_v = vb;
+    if (more) {
+      ids = after;
+      check(s + stride);
+      load_k();
+      next_v = vb + (g < 2 ? ids.x : ids.y) * page_elems;
+      after = step_pages(a, pt, s + 2 * stride);
+    }
+    uint4 hi[QT], lo[QT];
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
       if (left < kStep) {
 #pragma unroll
         for (int j = 0; j < 8; ++j)
-          if (8 * g + j >= left) p[j] = -INFINITY;
+          if (8 * g + j >= left) p[t][j] = -INFINITY;
       }
-      float mx = p[0];
+      float mx = p[t][0];
 #pragma unroll
-      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, p[j]);
+      for (int j = 1; j < 8; ++j) mx = fmaxf(mx, p[t][j]);
       mx = fmaxf(run.m[t], column_max(mx));
       if (__any(mx > run.m[t])) {  // seldom after the first steps
         const float c = run.m[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run.m[t] - mx);  // nothing to scale yet: 1
@@ -183,21 +209,31 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const He
       float sum = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
-        p[j] = __builtin_amdgcn_exp2f(p[j] - base);
-        sum += p[j];
+        p[t][j] = __builtin_amdgcn_exp2f(p[t][j] - base);
+        sum += p[t][j];
       }
       run.l[t] += sum;
-      uint4 hi, lo;
-      split_weights<T>(p, hi, lo);
-#pragma unroll
-      for (int i = 0; i < VC; ++i) {
-        run.o[t][i] = mfma<T>(v[i], hi, run.o[t][i]);
-        run.o[t][i] = mfma<T>(v[i], lo, run.o[t][i]);
-      }
+      split_weights<T>(p[t], hi[t], lo[t]);
     }
+    if (left < kStep) {  // slots past the length hold anything: 0 weights must multiply finite values
+      uint32_t keep[4];
+#pragma unroll
+      for (int d = 0; d < 4; ++d)
+        keep[d] = (8 * g + 2 * d < left ? 0xffffu : 0u) | (8 * g + 2 * d + 1 < left ? 0xffff0000u : 0u);
+#pragma unroll
+      for (int i = 0; i < VC; ++i) v[i] = make_uint4(v[i].x & keep[0], v[i].y & keep[1], v[i].z & keep[2], v[i].w & keep[3]);
+    }
+#pragma unroll
+    for (int i = 0; i < VC; ++i)
+#pragma unroll
+      for (int t = 0; t < QT; ++t) {
+        run.o[t][i] = mfma<T>(v[i], hi[t], run.o[t][i]);
+        run.o[t][i] = mfma<T>(v[i], lo[t], run.o[t][i]);
+      }
+    if (more) load_v(next_v);
   }
 #pragma unroll
-  for (int t = 0; t < QT; ++t) run.l[t] = column_sum(run.l[t]);
+  for (int t = 0; t < QT; ++t) run.l[t] = bad ? __builtin_nanf("") : column_sum(run.l[t]);
 }
 
 // Where the joined result of a head block goes: the output, or a partial (o fp32 [16 QT][HD], m and l [16 QT] each).
@@ -282,23 +318,28 @@ template <int HD, CacheType T, int QT, int W>
 __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a) {
   const int env = blockIdx.y, len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
   const HeadBlock b = head_block<QT>(a, blockIdx.x);
+  const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int2 ids = a.max_pages > 0 ? step_pages(a, a.page_table + env * a.ld_table, w) : make_int2(0, 0);
   if (steps == 0) return no_keys<HD, T>(a, env, b.head0, b.n, len);
   Running<HD, QT> run;
-  attend<HD, T, QT>(a, env, b, len, __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), steps, W, run);
+  attend<HD, T, QT>(a, env, b, len, w, steps, W, ids, run);
   join_waves<HD, T, QT, W>(a, env, b, run, {nullptr, nullptr});
 }
 
 // ------------------------------------------------------------------ split over the keys
 // The steps of all environments and head blocks lie in one line, environment by environment, head block by head block; a
-// persistent grid of workgroups takes equal runs of it.  A workgroup's first and last run of one (environment, head block)
-// may be a part of it: then it leaves a partial, in slot 2 w where an earlier workgroup began the line's piece, else in 2 w
-// + 1, and attn_join_kernel joins a piece's partials in order.  The line's start of every environment goes to the workspace.
-constexpr int kSplitGroups = 512, kSplitWaves = 4;
+// persistent grid of workgroups takes equal runs of it.  A workgroup's first and last piece (of one environment and head
+// block) may be a part: then it leaves a partial, in slot 2 w + 1 of the workspace if it began the piece, else in 2 w, and
+// who began a piece notes it down for attn_join_kernel, which adds its partials in order.
+template <int HD>
+constexpr int kSplitGroups = HD == 256 ? 256 : 512;
+constexpr int kSplitWaves = 4;
 constexpr int kSplitMinSteps = kSplitWaves;  // steps per workgroup at least
 
-__host__ __device__ __forceinline__ int split_workers(long long units) {
+template <int HD>
+__device__ __forceinline__ int split_workers(long long units) {
   const long long w = (units + kSplitMinSteps - 1) / kSplitMinSteps;
-  return w < kSplitGroups ? (int)w : kSplitGroups;
+  return w < kSplitGroups<HD> ? (int)w : kSplitGroups<HD>;
 }
 __device__ __forceinline__ long long worker_start(long long units, int workers, int w) { return units * w / workers; }
 // worker whose run holds unit u
@@ -307,54 +348,54 @@ __device__ __forceinline__ int worker_of(long long units, int workers, long long
 }
 
 struct SplitSpace {
-  long long* start;  // [n_env + 1] first unit of each environment
-  float* o;          // [2 kSplitGroups][16 QT][HD]
-  float* ml;         // [2 kSplitGroups][2][16 QT]
+  int4* begun;  // [groups] the piece that workgroup w began and did not end: environment, head block, last workgroup; or -1
+  float* o;     // [2 groups][16 QT][HD]
+  float* ml;    // [2 groups][2][16 QT]
 };
-size_t space_start_bytes(int n_env) { return ((size_t)(n_env + 1) * 8 + 255) / 256 * 256; }
 template <int HD, int QT>
-SplitSpace split_space(void* ws, int n_env) {
+SplitSpace split_space(void* ws) {
   char* p = static_cast<char*>(ws);
-  float* o = reinterpret_cast<float*>(p + space_start_bytes(n_env));
-  return {reinterpret_cast<long long*>(p), o, o + (size_t)2 * kSplitGroups * 16 * QT * HD};
+  float* o = reinterpret_cast<float*>(p + kSplitGroups<HD> * sizeof(int4));
+  return {reinterpret_cast<int4*>(p), o, o + (size_t)2 * kSplitGroups<HD> * 16 * QT * HD};
+}
+template <int HD>
+size_t split_bytes(int tiles) {
+  return kSplitGroups<HD> * (sizeof(int4) + (size_t)2 * 16 * tiles * (HD + 2) * sizeof(float));
 }
 
 template <int HD, CacheType T, int QT>
 __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnArgs a, SplitSpace sp, int blocks) {
   constexpr int NT = 64 * kSplitWaves;
-  __shared__ long long sums[NT];
+  __shared__ long long sums[kSplitWaves];
   __shared__ long long found_base;
   __shared__ int found_env;
-  const int tid = threadIdx.x, w = __builtin_amdgcn_readfirstlane(tid >> 6), me = blockIdx.x;
-  // every workgroup adds up the steps of all environments: thread t those of a run of them
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), me = blockIdx.x;
+  // every workgroup adds up the steps of all environments, thread t those of a run of them
   const int per = (a.n_env + NT - 1) / NT, e0 = min(a.n_env, tid * per), e1 = min(a.n_env, e0 + per);
   long long mine = 0;
   for (int e = e0; e < e1; ++e) mine += steps_of(a, a.lens[e]);
-  sums[tid] = mine;
+  long long upto = mine;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const long long v = __shfl_up(upto, o, kWave);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 63) sums[w] = upto;
   __syncthreads();
-  for (int o = 1; o < NT; o <<= 1) {
-    const long long v = tid >= o ? sums[tid - o] : 0;
-    __syncthreads();
-    sums[tid] += v;
-    __syncthreads();
+  long long units = 0;
+#pragma unroll
+  for (int i = 0; i < kSplitWaves; ++i) {
+    if (i < w) upto += sums[i];
+    units += sums[i];
   }
-  const long long units = sums[NT - 1] * blocks;
-  if (me == 0) {
-    long long at = (sums[tid] - mine) * blocks;
-    for (int e = e0; e < e1; ++e) {
-      sp.start[e] = at;
-      at += (long long)steps_of(a, a.lens[e]) * blocks;
-    }
-    if (tid == NT - 1) sp.start[a.n_env] = units;
-  }
-  const int workers = split_workers(units);
-  if (me >= workers) return;
-  long long u = worker_start(units, workers, me);
-  const long long u1 = worker_start(units, workers, me + 1), begin = u;
-  if (mine > 0 && (sums[tid] - mine) * blocks <= u && u < sums[tid] * blocks) {
-    long long at = (sums[tid] - mine) * blocks;
+  units *= blocks;
+  const int workers = split_workers<HD>(units);
+  long long u = me < workers ? worker_start(units, workers, me) : units;
+  const long long u1 = me < workers ? worker_start(units, workers, me + 1) : units, begin = u;
+  if ((upto - mine) * blocks <= u && u < upto * blocks) {
+    long long at = (upto - mine) * blocks;
     int e = e0;
-    for (;; ++e) {
+    for (; e < e1; ++e) {
       const long long n = (long long)steps_of(a, a.lens[e]) * blocks;
       if (u < at + n) break;
       at += n;
@@ -362,51 +403,57 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
     found_base = at;
     found_env = e;
   }
+  for (int e = me; e < a.n_env; e += kSplitGroups<HD>) {
+    const int len = a.lens[e];
+    if (steps_of(a, len) == 0) no_keys<HD, T>(a, e, 0, a.n_heads, len);
+  }
+  int4 begun = make_int4(-1, 0, 0, 0);
   __syncthreads();
-  long long base = found_base;
-  int env = __builtin_amdgcn_readfirstlane(found_env);
-  while (u < u1) {
-    const int len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
-    if (steps > 0) {
-      while (u < u1 && u < base + (long long)steps * blocks) {
-        const int hb = __builtin_amdgcn_readfirstlane((int)((u - base) / steps)), s0 = __builtin_amdgcn_readfirstlane((int)((u - base) % steps));
+  if (u < u1) {
+    long long base = found_base;
+    int env = __builtin_amdgcn_readfirstlane(found_env);
+    while (u < u1) {
+      const int len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
+      const long long end = base + (long long)steps * blocks;
+      while (u < u1 && u < end) {
+        const int hb = __builtin_amdgcn_readfirstlane((int)((unsigned)(u - base) / (unsigned)steps));
+        const int s0 = __builtin_amdgcn_readfirstlane((int)((u - base) - (long long)hb * steps));
         const int n = __builtin_amdgcn_readfirstlane((int)min((long long)(steps - s0), u1 - u));
         const HeadBlock b = head_block<QT>(a, hb);
+        const int2 ids = step_pages(a, a.page_table + env * a.ld_table, s0 + w);
         Running<HD, QT> run;
-        attend<HD, T, QT>(a, env, b, len, s0 + w, s0 + n, kSplitWaves, run);
+        attend<HD, T, QT>(a, env, b, len, s0 + w, s0 + n, kSplitWaves, ids, run);
         Partial part = {nullptr, nullptr};
         if (n < steps) {
-          const size_t slot = 2 * (size_t)me + (u - s0 < begin ? 0 : 1);
+          const bool began = u - s0 >= begin;
+          const size_t slot = 2 * (size_t)me + began;
           part = {sp.o + slot * 16 * QT * HD, sp.ml + slot * 2 * 16 * QT};
+          if (began) begun = make_int4(env, hb, worker_of(units, workers, u - s0 + steps - 1), 0);
         }
         __syncthreads();  // the last join's reads of LDS
         join_waves<HD, T, QT, kSplitWaves>(a, env, b, run, part);
         u += n;
       }
-      base += (long long)steps * blocks;
+      base = end;
+      ++env;
     }
-    ++env;
   }
+  if (tid == 0) sp.begun[me] = begun;
 }
 
-// One workgroup per (query head, environment): joins the partials of its head's keys, or writes the row of an environment
-// without steps; a piece that one workgroup held whole is done.
-constexpr int kJoinThreads = 512;
+// One workgroup per (workgroup of the split, row of a head block): joins the piece that it began.
+constexpr int kJoinThreads = 256;
 template <int HD, CacheType T, int QT>
-__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp, int blocks) {
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp) {
   constexpr int PG = kJoinThreads / HD;  // runs of partials added side by side
   __shared__ float so[PG][HD], sl[PG];
   __shared__ float sm[kJoinThreads / kWave];
-  const int head = blockIdx.x, env = blockIdx.y, tid = threadIdx.x;
-  const int len = a.lens[env], steps = steps_of(a, len);
-  if (steps == 0) return no_keys<HD, T>(a, env, head, 1, len);
-  const long long units = sp.start[a.n_env];
-  const int group = a.n_heads / a.n_kv_heads, hb = head / group * head_blocks<QT>(group) + head % group / (16 * QT);
-  const int row = head % group % (16 * QT), workers = split_workers(units);
-  const long long u0 = sp.start[env] + (long long)hb * steps, u1 = u0 + steps;
-  const int w0 = worker_of(units, workers, u0), w1 = worker_of(units, workers, u1 - 1);
-  if (w0 == w1) return;
-  // worker w0 began the piece; the others went on with it
+  const int w0 = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
+  const int4 piece = sp.begun[w0];
+  if (piece.x < 0) return;
+  const HeadBlock b = head_block<QT>(a, piece.y);
+  if (row >= b.n) return;
+  const int w1 = piece.z;
   auto slot = [&](int w) { return 2 * (size_t)w + (w == w0 ? 1 : 0); };
   float m = -INFINITY;
   for (int w = w0 + tid; w <= w1; w += kJoinThreads) m = fmaxf(m, sp.ml[slot(w) * 2 * 16 * QT + row]);
@@ -417,6 +464,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
   for (int i = 0; i < kJoinThreads / kWave; ++i) m = fmaxf(m, sm[i]);
   const int f = tid % HD, pg = tid / HD;
   float v = 0.f, l = 0.f;
+#pragma unroll 4
   for (int w = w0 + pg; w <= w1; w += PG) {
     const float* ml = sp.ml + slot(w) * 2 * 16 * QT;
     const float c = ml[row] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[row] - m);
@@ -433,8 +481,8 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
     v += so[i][f];
     l += sl[i];
   }
-  a.o[env * a.ld_o + (size_t)head * HD + f] = from_f32<T>(l == 0.f ? 0.f : v / l);
-  if (a.lse && f == 0) a.lse[(size_t)env * a.n_heads + head] = (m - kWeightExp<T> + __builtin_amdgcn_logf(l)) * kLn2;
+  a.o[piece.x * a.ld_o + (size_t)(b.head0 + row) * HD + f] = from_f32<T>(l == 0.f ? 0.f : v / l);
+  if (a.lse && f == 0) a.lse[(size_t)piece.x * a.n_heads + b.head0 + row] = (m - kWeightExp<T> + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 // ------------------------------------------------------------------ host
@@ -447,9 +495,10 @@ hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
   if (!split_keys(a.max_pages)) {
     hipLaunchKernelGGL((attn_whole_kernel<HD, T, QT, 4>), grid, dim3(256), 0, s, a);
   } else {
-    const SplitSpace sp = split_space<HD, QT>(a.ws, a.n_env);
-    hipLaunchKernelGGL((attn_split_kernel<HD, T, QT>), dim3(kSplitGroups), dim3(64 * kSplitWaves), 0, s, a, sp, blocks);
-    hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(a.n_heads, a.n_env), dim3(kJoinThreads), 0, s, a, sp, blocks);
+    const SplitSpace sp = split_space<HD, QT>(a.ws);
+    const int rows = std::min(16 * QT, a.n_heads / a.n_kv_heads);
+    hipLaunchKernelGGL((attn_split_kernel<HD, T, QT>), dim3(kSplitGroups<HD>), dim3(64 * kSplitWaves), 0, s, a, sp, blocks);
+    hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(kSplitGroups<HD>, rows), dim3(kJoinThreads), 0, s, a, sp);
   }
   return hipGetLastError();
 }
@@ -471,10 +520,10 @@ hipError_t launch_type(const PagedAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t paged_attn_bytes(int n_env, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
+size_t paged_attn_bytes(int, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
   if (!split_keys(max_pages)) return 256;
-  const size_t rows = 16 * query_tiles(n_heads, n_kv_heads);
-  return space_start_bytes(n_env) + (size_t)2 * kSplitGroups * rows * (head_dim + 2) * sizeof(float);
+  const int tiles = query_tiles(n_heads, n_kv_heads);
+  return head_dim == 64 ? split_bytes<64>(tiles) : head_dim == 128 ? split_bytes<128>(tiles) : split_bytes<256>(tiles);
 }
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
