@@ -13,6 +13,7 @@
 
 #include "cache.h"
 #include "common.h"
+#include "lds_limit.h"
 
 namespace vla {
 namespace {
@@ -61,6 +62,12 @@ __device__ __forceinline__ void split_weights(const float* p, uint4& hi, uint4& 
 // of it, where even 2^18 such keys do not show.
 template <CacheType T>
 constexpr float kWeightExp = T == kBf16 ? 0.f : 15.f;
+
+// log of the sum of weights l relative to the base-2 maximum m
+template <CacheType T>
+__device__ __forceinline__ float log_sum(float m, float l) {
+  return (m - kWeightExp<T> + __builtin_amdgcn_logf(l)) * kLn2;
+}
 
 // Max / sum over the lanes that share lane % 16.
 __device__ __forceinline__ float column_max(float v) {
@@ -242,59 +249,62 @@ struct Partial {
   float* ml;
 };
 
-// Joins the W waves' parts, 64 features at a time through LDS, and writes the output rows (part.o == null) or the partial.
+// LDS of the join of W waves: the rows of a head block, padded by one 16-byte bank group.
+template <int HD, int QT, int W>
+constexpr size_t kJoinBytes = (size_t)W * 16 * QT * (HD + 4 + 2) * sizeof(float);
+
+// Joins the W waves' parts through LDS and writes the output rows (part.o == null) or the partial.
 template <int HD, CacheType T, int QT, int W>
 __device__ __forceinline__ void join_waves(const PagedAttnArgs& a, int env, const HeadBlock& b, Running<HD, QT>& run, Partial part) {
-  constexpr int FS = 68;  // row of 64 features, padded
-  __shared__ float sm[W][16 * QT], sl[W][16 * QT];
-  __shared__ __align__(16) float so[W][16 * QT][FS];
+  extern __shared__ __align__(16) float lds[];
+  float* so = lds;                                  // [W][16 QT][HD + 4]
+  float* sm = lds + (size_t)W * 16 * QT * (HD + 4);  // [W][16 QT]
+  float* sl = sm + W * 16 * QT;
   const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m16 = lane & 15, g = lane >> 4;
-  if (g == 0) {
 #pragma unroll
-    for (int t = 0; t < QT; ++t) {
-      sm[w][16 * t + m16] = run.m[t];
-      sl[w][16 * t + m16] = run.l[t];
+  for (int t = 0; t < QT; ++t) {
+    const int h = w * 16 * QT + 16 * t + m16;
+    if (16 * t + m16 < b.n) {
+      if (g == 0) {
+        sm[h] = run.m[t];
+        sl[h] = run.l[t];
+      }
+#pragma unroll
+      for (int i = 0; i < HD / 16; ++i) *reinterpret_cast<f32x4*>(so + (size_t)h * (HD + 4) + 16 * i + 4 * g) = run.o[t][i];
     }
   }
   __syncthreads();
-  float scale[QT];
+  for (int i = tid; i < b.n * (HD / 4); i += 64 * W) {
+    const int h = i / (HD / 4), f = 4 * (i % (HD / 4));
+    float mu[W], m = -INFINITY, l = 0.f;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    float m = -INFINITY;
+    for (int u = 0; u < W; ++u) {
+      mu[u] = sm[u * 16 * QT + h];
+      m = fmaxf(m, mu[u]);
+    }
+    f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < W; ++u) m = fmaxf(m, sm[u][16 * t + m16]);
-    scale[t] = run.m[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run.m[t] - m);
-  }
+    for (int u = 0; u < W; ++u) {
+      const float c = mu[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mu[u] - m);  // a wave without keys adds zeros
+      l = fmaf(sl[u * 16 * QT + h], c, l);
+      const f32x4 o = *reinterpret_cast<const f32x4*>(so + (size_t)(u * 16 * QT + h) * (HD + 4) + f);
 #pragma unroll
-  for (int f0 = 0; f0 < HD / 64; ++f0) {
-    if (f0) __syncthreads();
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int t = 0; t < QT; ++t)
-        *reinterpret_cast<f32x4*>(&so[w][16 * t + m16][16 * i + 4 * g]) = run.o[t][4 * f0 + i] * scale[t];
-    __syncthreads();
-    for (int i = tid; i < b.n * 64; i += 64 * W) {
-      const int h = i / 64, f = i % 64;
-      float v = 0.f, m = -INFINITY, l = 0.f;
-#pragma unroll
-      for (int u = 0; u < W; ++u) {
-        v += so[u][h][f];
-        m = fmaxf(m, sm[u][h]);
+      for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], c, v[e]);
+    }
+    if (part.o) {
+      *reinterpret_cast<f32x4*>(part.o + h * HD + f) = v;
+      if (f == 0) {
+        part.ml[h] = m;
+        part.ml[16 * QT + h] = l;
       }
+    } else {
+      const float r = l == 0.f ? 0.f : 1.f / l;  // no key with a score above -inf: zeros
+      bf16_t h4[4];
 #pragma unroll
-      for (int u = 0; u < W; ++u) l += sl[u][h] * (sm[u][h] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(sm[u][h] - m));
-      if (part.o) {
-        part.o[h * HD + 64 * f0 + f] = v;
-        if (f0 == 0 && f == 0) {
-          part.ml[h] = m;
-          part.ml[16 * QT + h] = l;
-        }
-      } else {
-        a.o[env * a.ld_o + (size_t)(b.head0 + h) * HD + 64 * f0 + f] = from_f32<T>(l == 0.f ? 0.f : v / l);
-        if (a.lse && f0 == 0 && f == 0)
-          a.lse[(size_t)env * a.n_heads + b.head0 + h] = (m - kWeightExp<T> + __builtin_amdgcn_logf(l)) * kLn2;
-      }
+      for (int e = 0; e < 4; ++e) h4[e] = from_f32<T>(v[e] * r);
+      *reinterpret_cast<uint2*>(a.o + env * a.ld_o + (size_t)(b.head0 + h) * HD + f) =
+          make_uint2(h4[0] | (uint32_t)h4[1] << 16, h4[2] | (uint32_t)h4[3] << 16);
+      if (a.lse && f == 0) a.lse[(size_t)env * a.n_heads + b.head0 + h] = log_sum<T>(m, l);
     }
   }
 }
@@ -368,12 +378,13 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
   constexpr int NT = 64 * kSplitWaves;
   __shared__ long long sums[kSplitWaves];
   __shared__ long long found_base;
-  __shared__ int found_env;
+  __shared__ int found_env, found_len;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), me = blockIdx.x;
   // every workgroup adds up the steps of all environments, thread t those of a run of them
   const int per = (a.n_env + NT - 1) / NT, e0 = min(a.n_env, tid * per), e1 = min(a.n_env, e0 + per);
   long long mine = 0;
-  for (int e = e0; e < e1; ++e) mine += steps_of(a, a.lens[e]);
+  const int len0 = e0 < e1 ? a.lens[e0] : 0;
+  for (int e = e0; e < e1; ++e) mine += steps_of(a, e == e0 ? len0 : a.lens[e]);
   long long upto = mine;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -394,26 +405,24 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
   const long long u1 = me < workers ? worker_start(units, workers, me + 1) : units, begin = u;
   if ((upto - mine) * blocks <= u && u < upto * blocks) {
     long long at = (upto - mine) * blocks;
-    int e = e0;
-    for (; e < e1; ++e) {
-      const long long n = (long long)steps_of(a, a.lens[e]) * blocks;
+    int e = e0, len = len0;
+    for (;;) {
+      const long long n = (long long)steps_of(a, len) * blocks;
       if (u < at + n) break;
       at += n;
+      len = a.lens[++e];
     }
     found_base = at;
     found_env = e;
-  }
-  for (int e = me; e < a.n_env; e += kSplitGroups<HD>) {
-    const int len = a.lens[e];
-    if (steps_of(a, len) == 0) no_keys<HD, T>(a, e, 0, a.n_heads, len);
+    found_len = len;
   }
   int4 begun = make_int4(-1, 0, 0, 0);
   __syncthreads();
   if (u < u1) {
     long long base = found_base;
-    int env = __builtin_amdgcn_readfirstlane(found_env);
+    int env = __builtin_amdgcn_readfirstlane(found_env), len = __builtin_amdgcn_readfirstlane(found_len);
     while (u < u1) {
-      const int len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
+      const int steps = steps_of(a, len);
       const long long end = base + (long long)steps * blocks;
       while (u < u1 && u < end) {
         const int hb = __builtin_amdgcn_readfirstlane((int)((unsigned)(u - base) / (unsigned)steps));
@@ -435,71 +444,89 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
         u += n;
       }
       base = end;
-      ++env;
+      if (u < u1) len = __builtin_amdgcn_readfirstlane(a.lens[++env]);
     }
   }
   if (tid == 0) sp.begun[me] = begun;
+  for (int e = me; e < a.n_env; e += kSplitGroups<HD>) {
+    const int len = a.lens[e];
+    if (steps_of(a, len) == 0) no_keys<HD, T>(a, e, 0, a.n_heads, len);
+  }
 }
 
 // One workgroup per (workgroup of the split, row of a head block): joins the piece that it began.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 512;
 template <int HD, CacheType T, int QT>
 __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp) {
-  constexpr int PG = kJoinThreads / HD;  // runs of partials added side by side
-  __shared__ float so[PG][HD], sl[PG];
-  __shared__ float sm[kJoinThreads / kWave];
+  constexpr int PG = kJoinThreads / HD, NW = kJoinThreads / kWave;  // PG runs of partials are added side by side
+  static_assert(kSplitGroups<HD> <= kJoinThreads, "a partial per thread");
+  __shared__ float so[PG][HD], sc[kJoinThreads];
+  __shared__ float sm[NW], sl[NW];
   const int w0 = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   const int4 piece = sp.begun[w0];
   if (piece.x < 0) return;
   const HeadBlock b = head_block<QT>(a, piece.y);
   if (row >= b.n) return;
-  const int w1 = piece.z;
-  auto slot = [&](int w) { return 2 * (size_t)w + (w == w0 ? 1 : 0); };
-  float m = -INFINITY;
-  for (int w = w0 + tid; w <= w1; w += kJoinThreads) m = fmaxf(m, sp.ml[slot(w) * 2 * 16 * QT + row]);
+  const int parts = piece.z - w0 + 1;
+  auto slot = [&](int i) { return 2 * (size_t)(w0 + i) + (i == 0 ? 1 : 0); };
+  float m = -INFINITY, l = 0.f;
+  if (tid < parts) {
+    const float* ml = sp.ml + slot(tid) * 2 * 16 * QT;
+    m = ml[row];
+    l = ml[16 * QT + row];
+  }
+  const float mine = m;
   m = wave_max(m);
   if ((tid & 63) == 0) sm[tid >> 6] = m;
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < kJoinThreads / kWave; ++i) m = fmaxf(m, sm[i]);
+  for (int i = 0; i < NW; ++i) m = fmaxf(m, sm[i]);
+  const float c = mine == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine - m);
+  sc[tid] = c;
+  l = wave_sum(l * c);
+  if ((tid & 63) == 0) sl[tid >> 6] = l;
+  __syncthreads();
   const int f = tid % HD, pg = tid / HD;
-  float v = 0.f, l = 0.f;
-#pragma unroll 4
-  for (int w = w0 + pg; w <= w1; w += PG) {
-    const float* ml = sp.ml + slot(w) * 2 * 16 * QT;
-    const float c = ml[row] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(ml[row] - m);
-    v = fmaf(sp.o[slot(w) * 16 * QT * HD + row * HD + f], c, v);
-    l = fmaf(ml[16 * QT + row], c, l);
-  }
+  float v = 0.f;
+#pragma unroll 8
+  for (int i = pg; i < parts; i += PG) v = fmaf(sp.o[slot(i) * 16 * QT * HD + row * HD + f], sc[i], v);
   so[pg][f] = v;
-  if (f == 0) sl[pg] = l;
   __syncthreads();
   if (pg > 0) return;
   v = l = 0.f;
 #pragma unroll
-  for (int i = 0; i < PG; ++i) {
-    v += so[i][f];
-    l += sl[i];
-  }
+  for (int i = 0; i < PG; ++i) v += so[i][f];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) l += sl[i];
   a.o[piece.x * a.ld_o + (size_t)(b.head0 + row) * HD + f] = from_f32<T>(l == 0.f ? 0.f : v / l);
-  if (a.lse && f == 0) a.lse[(size_t)piece.x * a.n_heads + b.head0 + row] = (m - kWeightExp<T> + __builtin_amdgcn_logf(l)) * kLn2;
+  if (a.lse && f == 0) a.lse[(size_t)piece.x * a.n_heads + b.head0 + row] = log_sum<T>(m, l);
 }
 
 // ------------------------------------------------------------------ host
 bool split_keys(int max_pages) { return max_pages > 32; }
 
+template <int HD, CacheType T, int QT, int W>
+hipError_t launch_whole(const PagedAttnArgs& a, int blocks, hipStream_t s) {
+  static LdsLimit limit;
+  constexpr size_t lds = kJoinBytes<HD, QT, W>;
+  const hipError_t e = limit.allow((const void*)attn_whole_kernel<HD, T, QT, W>, lds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attn_whole_kernel<HD, T, QT, W>), dim3(blocks, a.n_env), dim3(64 * W), lds, s, a);
+  return hipGetLastError();
+}
+
 template <int HD, CacheType T, int QT>
 hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
   const int blocks = head_blocks<QT>(a.n_heads / a.n_kv_heads) * a.n_kv_heads;
-  const dim3 grid(blocks, a.n_env);
-  if (!split_keys(a.max_pages)) {
-    hipLaunchKernelGGL((attn_whole_kernel<HD, T, QT, 4>), grid, dim3(256), 0, s, a);
-  } else {
-    const SplitSpace sp = split_space<HD, QT>(a.ws);
-    const int rows = std::min(16 * QT, a.n_heads / a.n_kv_heads);
-    hipLaunchKernelGGL((attn_split_kernel<HD, T, QT>), dim3(kSplitGroups<HD>), dim3(64 * kSplitWaves), 0, s, a, sp, blocks);
-    hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(kSplitGroups<HD>, rows), dim3(kJoinThreads), 0, s, a, sp);
-  }
+  if (!split_keys(a.max_pages)) return launch_whole<HD, T, QT, 4>(a, blocks, s);
+  static LdsLimit limit;
+  constexpr size_t lds = kJoinBytes<HD, QT, kSplitWaves>;
+  const hipError_t e = limit.allow((const void*)attn_split_kernel<HD, T, QT>, lds);
+  if (e != hipSuccess) return e;
+  const SplitSpace sp = split_space<HD, QT>(a.ws);
+  const int rows = std::min(16 * QT, a.n_heads / a.n_kv_heads);
+  hipLaunchKernelGGL((attn_split_kernel<HD, T, QT>), dim3(kSplitGroups<HD>), dim3(64 * kSplitWaves), lds, s, a, sp, blocks);
+  hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(kSplitGroups<HD>, rows), dim3(kJoinThreads), 0, s, a, sp);
   return hipGetLastError();
 }
 
