@@ -132,15 +132,12 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const He
     for (int i = 0; i < VC; ++i) run.o[t][i] = {0.f, 0.f, 0.f, 0.f};
   }
   if (s0 >= s1) return;
-  uint4 q[QT][KC];
+  uint4 q[QT][KC];  // columns past the block's heads repeat its last one; nothing reads what becomes of them
 #pragma unroll
   for (int t = 0; t < QT; ++t)
 #pragma unroll
-    for (int i = 0; i < KC; ++i) {
-      q[t][i] = make_uint4(0, 0, 0, 0);
-      if (16 * t + m16 < b.n)
-        q[t][i] = *reinterpret_cast<const uint4*>(a.q + env * a.ld_q + (size_t)(b.head0 + 16 * t + m16) * HD + 32 * i + 8 * g);
-    }
+    for (int i = 0; i < KC; ++i)
+      q[t][i] = *reinterpret_cast<const uint4*>(a.q + env * a.ld_q + (size_t)(b.head0 + min(16 * t + m16, b.n - 1)) * HD + 32 * i + 8 * g);
   const int32_t* pt = a.page_table + env * a.ld_table;
   const int last = (len - 1) / kPage;
   const size_t page_elems = (size_t)a.n_kv_heads * kPage * HD;
@@ -172,8 +169,8 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const He
   load_v(vb + (g < 2 ? ids.x : ids.y) * page_elems);
   int2 after = step_pages(a, pt, s0 + stride);  // of the next step
   for (int s = s0; s < s1; s += stride) {
-    const int left = len - kStep * s;  // keys of the step that count
     const bool more = s + stride < s1;
+    const int left = len - kStep * s;  // keys of the step that count
     float p[QT][8];
 #pragma unroll
     for (int t = 0; t < QT; ++t)
@@ -338,23 +335,18 @@ __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a) {
 
 // ------------------------------------------------------------------ split over the keys
 // The steps of all environments and head blocks lie in one line, environment by environment, head block by head block; a
-// persistent grid of workgroups takes equal runs of it.  A workgroup's first and last piece (of one environment and head
+// persistent grid of workgroups takes runs of equal length.  A workgroup's first and last piece (of one environment and head
 // block) may be a part: then it leaves a partial, in slot 2 w + 1 of the workspace if it began the piece, else in 2 w, and
 // who began a piece notes it down for attn_join_kernel, which adds its partials in order.
 template <int HD>
 constexpr int kSplitGroups = HD == 256 ? 256 : 512;
 constexpr int kSplitWaves = 4;
-constexpr int kSplitMinSteps = kSplitWaves;  // steps per workgroup at least
 
+// Units of a workgroup: whole rounds of its waves.
 template <int HD>
-__device__ __forceinline__ int split_workers(long long units) {
-  const long long w = (units + kSplitMinSteps - 1) / kSplitMinSteps;
-  return w < kSplitGroups<HD> ? (int)w : kSplitGroups<HD>;
-}
-__device__ __forceinline__ long long worker_start(long long units, int workers, int w) { return units * w / workers; }
-// worker whose run holds unit u
-__device__ __forceinline__ int worker_of(long long units, int workers, long long u) {
-  return (int)(((u + 1) * workers + units - 1) / units) - 1;
+__device__ __forceinline__ long long units_per_group(long long units) {
+  const long long n = (units + kSplitGroups<HD> - 1) / kSplitGroups<HD>;
+  return max((n + kSplitWaves - 1) / kSplitWaves, 1ll) * kSplitWaves;
 }
 
 struct SplitSpace {
@@ -400,9 +392,8 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
     units += sums[i];
   }
   units *= blocks;
-  const int workers = split_workers<HD>(units);
-  long long u = me < workers ? worker_start(units, workers, me) : units;
-  const long long u1 = me < workers ? worker_start(units, workers, me + 1) : units, begin = u;
+  const long long per_group = units_per_group<HD>(units), begin = min(me * per_group, units), u1 = min(begin + per_group, units);
+  long long u = begin;
   if ((upto - mine) * blocks <= u && u < upto * blocks) {
     long long at = (upto - mine) * blocks;
     int e = e0, len = len0;
@@ -437,7 +428,7 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
           const bool began = u - s0 >= begin;
           const size_t slot = 2 * (size_t)me + began;
           part = {sp.o + slot * 16 * QT * HD, sp.ml + slot * 2 * 16 * QT};
-          if (began) begun = make_int4(env, hb, worker_of(units, workers, u - s0 + steps - 1), 0);
+          if (began) begun = make_int4(env, hb, me + (int)((unsigned)(u - s0 + steps - 1 - begin) / (unsigned)per_group), 0);
         }
         __syncthreads();  // the last join's reads of LDS
         join_waves<HD, T, QT, kSplitWaves>(a, env, b, run, part);
@@ -455,13 +446,14 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
 }
 
 // One workgroup per (workgroup of the split, row of a head block): joins the piece that it began.
-constexpr int kJoinThreads = 512;
+constexpr int kJoinThreads = 256;
 template <int HD, CacheType T, int QT>
 __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp) {
-  constexpr int PG = kJoinThreads / HD, NW = kJoinThreads / kWave;  // PG runs of partials are added side by side
-  static_assert(kSplitGroups<HD> <= kJoinThreads, "a partial per thread");
-  __shared__ float so[PG][HD], sc[kJoinThreads];
-  __shared__ float sm[NW], sl[NW];
+  constexpr int PG = kJoinThreads * 4 / HD, NW = kJoinThreads / kWave;  // PG runs of partials are added side by side
+  constexpr int PT = kSplitGroups<HD> / kJoinThreads;                   // partials per thread
+  static_assert(kSplitGroups<HD> % kJoinThreads == 0, "partials are dealt out evenly");
+  __shared__ __align__(16) float so[PG][HD];
+  __shared__ float sc[kSplitGroups<HD>], sm[NW], sl[NW];
   const int w0 = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   const int4 piece = sp.begun[w0];
   if (piece.x < 0) return;
@@ -469,37 +461,54 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
   if (row >= b.n) return;
   const int parts = piece.z - w0 + 1;
   auto slot = [&](int i) { return 2 * (size_t)(w0 + i) + (i == 0 ? 1 : 0); };
-  float m = -INFINITY, l = 0.f;
-  if (tid < parts) {
-    const float* ml = sp.ml + slot(tid) * 2 * 16 * QT;
-    m = ml[row];
-    l = ml[16 * QT + row];
+  float mp[PT], lp[PT], m = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int j = 0; j < PT; ++j) {
+    const int i = tid + j * kJoinThreads;
+    mp[j] = -INFINITY;
+    lp[j] = 0.f;
+    if (i < parts) {
+      const float* ml = sp.ml + slot(i) * 2 * 16 * QT;
+      mp[j] = ml[row];
+      lp[j] = ml[16 * QT + row];
+    }
+    m = fmaxf(m, mp[j]);
   }
-  const float mine = m;
   m = wave_max(m);
   if ((tid & 63) == 0) sm[tid >> 6] = m;
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < NW; ++i) m = fmaxf(m, sm[i]);
-  const float c = mine == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mine - m);
-  sc[tid] = c;
-  l = wave_sum(l * c);
+#pragma unroll
+  for (int j = 0; j < PT; ++j) {
+    const float c = mp[j] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mp[j] - m);
+    sc[tid + j * kJoinThreads] = c;
+    l = fmaf(lp[j], c, l);
+  }
+  l = wave_sum(l);
   if ((tid & 63) == 0) sl[tid >> 6] = l;
   __syncthreads();
-  const int f = tid % HD, pg = tid / HD;
-  float v = 0.f;
+  const int f = 4 * (tid % (HD / 4)), pg = tid / (HD / 4);
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
-  for (int i = pg; i < parts; i += PG) v = fmaf(sp.o[slot(i) * 16 * QT * HD + row * HD + f], sc[i], v);
-  so[pg][f] = v;
-  __syncthreads();
-  if (pg > 0) return;
-  v = l = 0.f;
+  for (int i = pg; i < parts; i += PG) {
+    const f32x4 o = *reinterpret_cast<const f32x4*>(sp.o + slot(i) * 16 * QT * HD + row * HD + f);
 #pragma unroll
-  for (int i = 0; i < PG; ++i) v += so[i][f];
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], sc[i], v[e]);
+  }
+  *reinterpret_cast<f32x4*>(&so[pg][f]) = v;
+  __syncthreads();
+  l = 0.f;
 #pragma unroll
   for (int i = 0; i < NW; ++i) l += sl[i];
-  a.o[piece.x * a.ld_o + (size_t)(b.head0 + row) * HD + f] = from_f32<T>(l == 0.f ? 0.f : v / l);
-  if (a.lse && f == 0) a.lse[(size_t)piece.x * a.n_heads + b.head0 + row] = log_sum<T>(m, l);
+  const float r = l == 0.f ? 0.f : 1.f / l;
+  if (tid < HD) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < PG; ++i) t += so[i][tid];
+    a.o[piece.x * a.ld_o + (size_t)(b.head0 + row) * HD + tid] = from_f32<T>(t * r);
+  }
+  if (a.lse && tid == 0) a.lse[(size_t)piece.x * a.n_heads + b.head0 + row] = log_sum<T>(m, l);
 }
 
 // ------------------------------------------------------------------ host
@@ -530,12 +539,15 @@ hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-// Query heads of a group by tiles of 16: two share a step's keys in registers, more read them again.
-int query_tiles(int n_heads, int n_kv_heads) { return n_heads / n_kv_heads > 16 ? 2 : 1; }
+// Query heads of a group by tiles of 16: up to head_dim 128 two share a step's keys in registers (at 256 two tiles' sums do
+// not fit), further ones read the keys again.
+int query_tiles(int n_heads, int n_kv_heads, int head_dim) { return head_dim < 256 && n_heads / n_kv_heads > 16 ? 2 : 1; }
 
 template <int HD, CacheType T>
 hipError_t launch_heads(const PagedAttnArgs& a, hipStream_t s) {
-  return query_tiles(a.n_heads, a.n_kv_heads) == 1 ? launch_blocks<HD, T, 1>(a, s) : launch_blocks<HD, T, 2>(a, s);
+  if constexpr (HD < 256)
+    if (query_tiles(a.n_heads, a.n_kv_heads, HD) == 2) return launch_blocks<HD, T, 2>(a, s);
+  return launch_blocks<HD, T, 1>(a, s);
 }
 template <CacheType T>
 hipError_t launch_type(const PagedAttnArgs& a, hipStream_t s) {
@@ -549,7 +561,7 @@ hipError_t launch_type(const PagedAttnArgs& a, hipStream_t s) {
 
 size_t paged_attn_bytes(int, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
   if (!split_keys(max_pages)) return 256;
-  const int tiles = query_tiles(n_heads, n_kv_heads);
+  const int tiles = query_tiles(n_heads, n_kv_heads, head_dim);
   return head_dim == 64 ? split_bytes<64>(tiles) : head_dim == 128 ? split_bytes<128>(tiles) : split_bytes<256>(tiles);
 }
 
