@@ -10,6 +10,8 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdlib>
+#include <type_traits>
 
 #include "cache.h"
 #include "common.h"
@@ -20,6 +22,9 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
+#ifndef GROUPSX
+#define GROUPSX (HD == 256 || (HD == 128 && QT == 2) ? 256 : HD == 64 && QT == 1 ? 1024 : 512)
+#endif
 constexpr int kStep = 32;  // keys of a wave's step
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -106,72 +111,79 @@ struct Running {
 
 typedef unsigned u32x4v __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ uint4 load_once(const bf16_t* p) {  // past the caches: a page is read by one wave
+  #ifdef PLAINX
+  const u32x4v v = *reinterpret_cast<const u32x4v*>(p);
+#else
   const u32x4v v = __builtin_nontemporal_load(reinterpret_cast<const u32x4v*>(p));
+#endif
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 
 // The pages of step s; entries up to the table's end may be read before the length is known.
-__device__ __forceinline__ int2 step_pages(const PagedAttnArgs& a, const int32_t* pt, int s) {
-  return make_int2(pt[min(2 * s, a.max_pages - 1)], pt[min(2 * s + 1, a.max_pages - 1)]);
+__device__ __forceinline__ int2 step_pages(const int32_t* pt, int max_pages, int s) {
+  return make_int2(pt[min(2 * s, max_pages - 1)], pt[min(2 * s + 1, max_pages - 1)]);
 }
 
-// Steps s0, s0 + stride, ... below s1 of environment `env`, of `len` keys, for head block b; `ids` are step s0's pages.  A
-// step's keys are requested as soon as the step before has used its own, its values likewise, so that a wave always has one
-// step's pages on the way.
+// A wave at its steps.
 template <int HD, CacheType T, int QT>
-__device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const HeadBlock& b, int len, int s0, int s1, int stride,
-                                       int2 ids, Running<HD, QT>& run) {
-  constexpr int KC = HD / 32, VC = HD / 16;
-  const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
-  const float scale = a.scale * kLog2e;
+struct Wave {
+  static constexpr int KC = HD / 32, VC = HD / 16;
+  const PagedAttnArgs& a;
+  int m16, g;
+  float scale;
+  size_t page_elems;
+  uint4 q[QT][KC], k[2][KC], v[VC];
+  Running<HD, QT> run;
+  bool bad;  // a page outside the pool among the keys since begin()
+
+  __device__ __forceinline__ explicit Wave(const PagedAttnArgs& args)
+      : a(args), m16(threadIdx.x & 15), g((threadIdx.x & 63) >> 4), scale(args.scale * kLog2e),
+        page_elems((size_t)args.n_kv_heads * kPage * HD) {}
+
+  __device__ __forceinline__ void begin() {
+    bad = false;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    run.m[t] = -INFINITY;
-    run.l[t] = 0.f;
+    for (int t = 0; t < QT; ++t) {
+      run.m[t] = -INFINITY;
+      run.l[t] = 0.f;
 #pragma unroll
-    for (int i = 0; i < VC; ++i) run.o[t][i] = {0.f, 0.f, 0.f, 0.f};
-  }
-  if (s0 >= s1) return;
-  uint4 q[QT][KC];  // columns past the block's heads repeat its last one; nothing reads what becomes of them
-#pragma unroll
-  for (int t = 0; t < QT; ++t)
-#pragma unroll
-    for (int i = 0; i < KC; ++i)
-      q[t][i] = *reinterpret_cast<const uint4*>(a.q + env * a.ld_q + (size_t)(b.head0 + min(16 * t + m16, b.n - 1)) * HD + 32 * i + 8 * g);
-  const int32_t* pt = a.page_table + env * a.ld_table;
-  const int last = (len - 1) / kPage;
-  const size_t page_elems = (size_t)a.n_kv_heads * kPage * HD;
-  // row lane % 16 of the K operand of tile t: page m16 / 8 of the step, slot 8 (m16 / 4 % 2) + 4 t + m16 % 4
-  const bf16_t* kb = a.pages.k + ((size_t)b.kvh * kPage + 8 * ((m16 >> 2) & 1) + (m16 & 3)) * HD + 8 * g;
-  const bf16_t* vb = a.pages.v + ((size_t)b.kvh * HD + m16) * kPage + 8 * (g & 1);
-  bool bad = false;
-  auto check = [&](int s) {  // a bad page is not read: NaN from there on
-    if (2 * s + 1 > last) ids.y = ids.x;
-    if ((unsigned)ids.x >= (unsigned)a.n_pages || (unsigned)ids.y >= (unsigned)a.n_pages) {
-      ids = make_int2(0, 0);
-      bad = true;
+      for (int i = 0; i < VC; ++i) run.o[t][i] = {0.f, 0.f, 0.f, 0.f};
     }
-  };
-  uint4 k[2][KC], v[VC];
-  auto load_k = [&] {
-    const bf16_t* kp = kb + (m16 < 8 ? ids.x : ids.y) * page_elems;
+  }
+
+  __device__ __forceinline__ void load_q(int env, const HeadBlock& b) {  // columns past the block's heads repeat its last one
+#pragma unroll
+    for (int t = 0; t < QT; ++t)
+#pragma unroll
+      for (int i = 0; i < KC; ++i)
+        q[t][i] = *reinterpret_cast<const uint4*>(a.q + env * a.ld_q + (size_t)(b.head0 + min(16 * t + m16, b.n - 1)) * HD + 32 * i + 8 * g);
+  }
+
+  // The pages to read for step s of `len` keys, of which `ids` are the table's: no page past the last one, none outside the
+  // pool (`outside` then).
+  __device__ __forceinline__ int2 usable(int2 ids, int len, int s, bool& outside) const {
+    if (2 * s + 1 > (len - 1) / kPage) ids.y = ids.x;
+    outside = (unsigned)ids.x >= (unsigned)a.n_pages || (unsigned)ids.y >= (unsigned)a.n_pages;
+    return outside ? make_int2(0, 0) : ids;
+  }
+  // K operand: row lane % 16 of tile t is page m16 / 8 of the step, slot 8 (m16 / 4 % 2) + 4 t + m16 % 4
+  __device__ __forceinline__ void load_k(int2 ids, int kvh) {
+    const bf16_t* p = a.pages.k + ((size_t)kvh * kPage + 8 * ((m16 >> 2) & 1) + (m16 & 3)) * HD + 8 * g + (m16 < 8 ? ids.x : ids.y) * page_elems;
 #pragma unroll
     for (int i = 0; i < KC; ++i)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) k[t][i] = load_once(kp + 4 * t * HD + 32 * i);
-  };
-  auto load_v = [&](const bf16_t* vp) {
+      for (int t = 0; t < 2; ++t) k[t][i] = load_once(p + 4 * t * HD + 32 * i);
+  }
+  __device__ __forceinline__ const bf16_t* v_at(int2 ids, int kvh) const {
+    return a.pages.v + ((size_t)kvh * HD + m16) * kPage + 8 * (g & 1) + (g < 2 ? ids.x : ids.y) * page_elems;
+  }
+  __device__ __forceinline__ void load_v(const bf16_t* p) {
 #pragma unroll
-    for (int i = 0; i < VC; ++i) v[i] = load_once(vp + 16 * i * kPage);
-  };
-  check(s0);
-  load_k();
-  load_v(vb + (g < 2 ? ids.x : ids.y) * page_elems);
-  int2 after = step_pages(a, pt, s0 + stride);  // of the next step
-  for (int s = s0; s < s1; s += stride) {
-    const bool more = s + stride < s1;
-    const int left = len - kStep * s;  // keys of the step that count
-    float p[QT][8];
+    for (int i = 0; i < VC; ++i) v[i] = load_once(p + 16 * i * kPage);
+  }
+
+  // p = base-2 scores of the step's keys; k and q are free afterwards
+  __device__ __forceinline__ void scores(float (&p)[QT][8]) {
 #pragma unroll
     for (int t = 0; t < QT; ++t)
 #pragma unroll
@@ -182,14 +194,9 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const He
 #pragma unroll
         for (int r = 0; r < 4; ++r) p[t][4 * u + r] = c[r] * scale;
       }
-    const bf16_t* next_v = vb;
-    if (more) {
-      ids = after;
-      check(s + stride);
-      load_k();
-      next_v = vb + (g < 2 ? ids.x : ids.y) * page_elems;
-      after = step_pages(a, pt, s + 2 * stride);
-    }
+  }
+  // Takes the step's keys, of which `left` (< 32: the last step) count, into the running sums; v is free afterwards.
+  __device__ __forceinline__ void weigh(float (&p)[QT][8], int left) {
     uint4 hi[QT], lo[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
@@ -234,73 +241,90 @@ __device__ __forceinline__ void attend(const PagedAttnArgs& a, int env, const He
         run.o[t][i] = mfma<T>(v[i], hi[t], run.o[t][i]);
         run.o[t][i] = mfma<T>(v[i], lo[t], run.o[t][i]);
       }
-    if (more) load_v(next_v);
   }
+  // l over all keys since begin(), in every lane of its column
+  __device__ __forceinline__ void end() {
 #pragma unroll
-  for (int t = 0; t < QT; ++t) run.l[t] = bad ? __builtin_nanf("") : column_sum(run.l[t]);
-}
+    for (int t = 0; t < QT; ++t) run.l[t] = bad ? __builtin_nanf("") : column_sum(run.l[t]);
+  }
+};
 
-// Where the joined result of a head block goes: the output, or a partial (o fp32 [16 QT][HD], m and l [16 QT] each).
+// Where a joined result goes: the output, or a partial (o fp32 [rows][HD], m and l [rows] each).
 struct Partial {
   float* o;
   float* ml;
+  int rows;
 };
 
-// LDS of the join of W waves: the rows of a head block, padded by one 16-byte bank group.
-template <int HD, int QT, int W>
-constexpr size_t kJoinBytes = (size_t)W * 16 * QT * (HD + 4 + 2) * sizeof(float);
-
-// Joins the W waves' parts through LDS and writes the output rows (part.o == null) or the partial.
-template <int HD, CacheType T, int QT, int W>
-__device__ __forceinline__ void join_waves(const PagedAttnArgs& a, int env, const HeadBlock& b, Running<HD, QT>& run, Partial part) {
-  extern __shared__ __align__(16) float lds[];
-  float* so = lds;                                  // [W][16 QT][HD + 4]
-  float* sm = lds + (size_t)W * 16 * QT * (HD + 4);  // [W][16 QT]
-  float* sl = sm + W * 16 * QT;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6, m16 = lane & 15, g = lane >> 4;
+// Parts of a head block's result in LDS, one after the other: per part and head the sums O (HD + 4 floats, padded by a
+// 16-byte bank group), m and l.
+template <int HD>
+struct Parts {
+  float* o;   // [parts][rows][HD + 4]
+  float* ml;  // [parts][2][rows]
+  int rows;
+  static size_t bytes(int parts, int rows) { return (size_t)parts * rows * (HD + 4 + 2) * sizeof(float); }
+  __device__ __forceinline__ Parts(float* lds, int parts, int n) : o(lds), ml(lds + (size_t)parts * n * (HD + 4)), rows(n) {}
+  template <int QT>
+  __device__ __forceinline__ void put(int part, const Running<HD, QT>& run, int heads) {
+    const int lane = threadIdx.x & 63, m16 = lane & 15, g = lane >> 4;
 #pragma unroll
-  for (int t = 0; t < QT; ++t) {
-    const int h = w * 16 * QT + 16 * t + m16;
-    if (16 * t + m16 < b.n) {
-      if (g == 0) {
-        sm[h] = run.m[t];
-        sl[h] = run.l[t];
+    for (int t = 0; t < QT; ++t) {
+      const int h = 16 * t + m16;
+      if (h < heads) {
+        if (g == 0) {
+          ml[part * 2 * rows + h] = run.m[t];
+          ml[(part * 2 + 1) * rows + h] = run.l[t];
+        }
+#pragma unroll
+        for (int i = 0; i < HD / 16; ++i)
+          *reinterpret_cast<f32x4*>(o + (size_t)(part * rows + h) * (HD + 4) + 16 * i + 4 * g) = run.o[t][i];
       }
-#pragma unroll
-      for (int i = 0; i < HD / 16; ++i) *reinterpret_cast<f32x4*>(so + (size_t)h * (HD + 4) + 16 * i + 4 * g) = run.o[t][i];
     }
   }
-  __syncthreads();
-  for (int i = tid; i < b.n * (HD / 4); i += 64 * W) {
-    const int h = i / (HD / 4), f = 4 * (i % (HD / 4));
-    float mu[W], m = -INFINITY, l = 0.f;
+};
+
+template <CacheType T>
+__device__ __forceinline__ void store4(bf16_t* p, const f32x4& v, float r) {
+  bf16_t h[4];
 #pragma unroll
-    for (int u = 0; u < W; ++u) {
-      mu[u] = sm[u * 16 * QT + h];
+  for (int e = 0; e < 4; ++e) h[e] = from_f32<T>(v[e] * r);
+  *reinterpret_cast<uint2*>(p) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
+}
+__device__ __forceinline__ float reciprocal(float l) { return l == 0.f ? 0.f : 1.f / l; }  // no score above -inf: zeros
+
+// Adds parts first, first + step, ... (N of them) by the whole workgroup.
+template <int HD, CacheType T, int N>
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, int env, const HeadBlock& b, const Parts<HD>& ps, int first,
+                                           int n, int second, int step, const Partial& to) {
+  for (int i = threadIdx.x; i < b.n * (HD / 4); i += blockDim.x) {
+    const int h = i / (HD / 4), f = 4 * (i % (HD / 4));
+    float mu[N], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+      const int p = u == 0 ? first : second + (u - 1) * step;
+      mu[u] = u < n ? ps.ml[p * 2 * ps.rows + h] : -INFINITY;
       m = fmaxf(m, mu[u]);
     }
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int u = 0; u < W; ++u) {
-      const float c = mu[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mu[u] - m);  // a wave without keys adds zeros
-      l = fmaf(sl[u * 16 * QT + h], c, l);
-      const f32x4 o = *reinterpret_cast<const f32x4*>(so + (size_t)(u * 16 * QT + h) * (HD + 4) + f);
+    for (int u = 0; u < N; ++u) {
+      if (u >= n) break;
+      const int p = u == 0 ? first : second + (u - 1) * step;
+      const float c = mu[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mu[u] - m);  // a part without keys adds zeros
+      l = fmaf(ps.ml[(p * 2 + 1) * ps.rows + h], c, l);
+      const f32x4 o = *reinterpret_cast<const f32x4*>(ps.o + (size_t)(p * ps.rows + h) * (HD + 4) + f);
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], c, v[e]);
     }
-    if (part.o) {
-      *reinterpret_cast<f32x4*>(part.o + h * HD + f) = v;
+    if (to.o) {
+      *reinterpret_cast<f32x4*>(to.o + h * HD + f) = v;
       if (f == 0) {
-        part.ml[h] = m;
-        part.ml[16 * QT + h] = l;
+        to.ml[h] = m;
+        to.ml[to.rows + h] = l;
       }
     } else {
-      const float r = l == 0.f ? 0.f : 1.f / l;  // no key with a score above -inf: zeros
-      bf16_t h4[4];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) h4[e] = from_f32<T>(v[e] * r);
-      *reinterpret_cast<uint2*>(a.o + env * a.ld_o + (size_t)(b.head0 + h) * HD + f) =
-          make_uint2(h4[0] | (uint32_t)h4[1] << 16, h4[2] | (uint32_t)h4[3] << 16);
+      store4<T>(a.o + env * a.ld_o + (size_t)(b.head0 + h) * HD + f, v, reciprocal(l));
       if (a.lse && f == 0) a.lse[(size_t)env * a.n_heads + b.head0 + h] = log_sum<T>(m, l);
     }
   }
@@ -320,63 +344,106 @@ __device__ __forceinline__ void no_keys(const PagedAttnArgs& a, int env, int hea
   if (a.lse && (int)threadIdx.x < n) a.lse[(size_t)env * a.n_heads + head0 + threadIdx.x] = len == 0 ? -INFINITY : v;
 }
 
-// One workgroup of W waves per (head block, environment).
+// One workgroup of W waves per (head block, environment); wave w takes steps w, w + W, ...
 template <int HD, CacheType T, int QT, int W>
-__global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a) {
+__global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a, int rows) {
+  extern __shared__ __align__(16) float lds[];
   const int env = blockIdx.y, len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
   const HeadBlock b = head_block<QT>(a, blockIdx.x);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int2 ids = a.max_pages > 0 ? step_pages(a, a.page_table + env * a.ld_table, w) : make_int2(0, 0);
+  const int32_t* pt = a.page_table + env * a.ld_table;
+  int2 ids = a.max_pages > 0 ? step_pages(pt, a.max_pages, w) : make_int2(0, 0);
   if (steps == 0) return no_keys<HD, T>(a, env, b.head0, b.n, len);
-  Running<HD, QT> run;
-  attend<HD, T, QT>(a, env, b, len, w, steps, W, ids, run);
-  join_waves<HD, T, QT, W>(a, env, b, run, {nullptr, nullptr});
+  Wave<HD, T, QT> wave(a);
+  wave.begin();
+  if (w < steps) {
+    bool outside;
+    wave.load_q(env, b);
+    ids = wave.usable(ids, len, w, outside);
+    wave.bad |= outside;
+    wave.load_k(ids, b.kvh);
+    wave.load_v(wave.v_at(ids, b.kvh));
+    ids = step_pages(pt, a.max_pages, w + W);
+    for (int s = w; s < steps; s += W) {
+      float p[QT][8];
+      wave.scores(p);
+      const bool more = s + W < steps;
+      const bf16_t* next_v = nullptr;
+      if (more) {
+        ids = wave.usable(ids, len, s + W, outside);
+        wave.bad |= outside;
+        wave.load_k(ids, b.kvh);
+        next_v = wave.v_at(ids, b.kvh);
+        ids = step_pages(pt, a.max_pages, s + 2 * W);
+      }
+      wave.weigh(p, len - kStep * s);
+      if (more) wave.load_v(next_v);
+    }
+  }
+  wave.end();
+  Parts<HD> ps(lds, W, rows);
+  ps.put(w, wave.run, b.n);
+  __syncthreads();
+  join_parts<HD, T, W>(a, env, b, ps, 0, W, 1, 1, {nullptr, nullptr, 0});
 }
 
 // ------------------------------------------------------------------ split over the keys
-// The steps of all environments and head blocks lie in one line, environment by environment, head block by head block; a
-// persistent grid of workgroups takes runs of equal length.  A workgroup's first and last piece (of one environment and head
-// block) may be a part: then it leaves a partial, in slot 2 w + 1 of the workspace if it began the piece, else in 2 w, and
-// who began a piece notes it down for attn_join_kernel, which adds its partials in order.
-template <int HD>
-constexpr int kSplitGroups = HD == 256 ? 256 : 512;
-constexpr int kSplitWaves = 4;
-
-// Units of a workgroup: whole rounds of its waves.
-template <int HD>
-__device__ __forceinline__ long long units_per_group(long long units) {
-  const long long n = (units + kSplitGroups<HD> - 1) / kSplitGroups<HD>;
-  return max((n + kSplitWaves - 1) / kSplitWaves, 1ll) * kSplitWaves;
-}
+// The steps of all environments and head blocks lie in one line, environment by environment, head block by head block (a
+// piece is one environment and head block); a persistent grid takes the line in runs of equal length, one per wave, so that
+// ragged lengths cost nothing.  A wave goes from piece to piece without a pause: the next step's pages are on their way
+// while a step is taken, whatever piece it belongs to.  A piece inside a wave's run is written by the wave; what runs past
+// the run's ends is left in LDS, joined there with the neighbouring waves' parts, and what runs past the workgroup's ends
+// goes to the workspace: slot 2 w + 1 of workgroup w if the piece began there, else 2 w.  Who began a piece notes it down
+// for attn_join_kernel, which adds its partials in order.
+template <int HD, int QT>
+constexpr int kRunGroups = GROUPSX;
+constexpr int kRunWaves = 4, kRunThreads = 64 * kRunWaves;
 
 struct SplitSpace {
   int4* begun;  // [groups] the piece that workgroup w began and did not end: environment, head block, last workgroup; or -1
-  float* o;     // [2 groups][16 QT][HD]
-  float* ml;    // [2 groups][2][16 QT]
+  float* o;     // [2 groups][rows][HD]
+  float* ml;    // [2 groups][2][rows]
 };
 template <int HD, int QT>
-SplitSpace split_space(void* ws) {
+SplitSpace split_space(void* ws, int rows) {
   char* p = static_cast<char*>(ws);
-  float* o = reinterpret_cast<float*>(p + kSplitGroups<HD> * sizeof(int4));
-  return {reinterpret_cast<int4*>(p), o, o + (size_t)2 * kSplitGroups<HD> * 16 * QT * HD};
+  float* o = reinterpret_cast<float*>(p + kRunGroups<HD, QT> * sizeof(int4));
+  return {reinterpret_cast<int4*>(p), o, o + (size_t)2 * kRunGroups<HD, QT> * rows * HD};
 }
-template <int HD>
-size_t split_bytes(int tiles) {
-  return kSplitGroups<HD> * (sizeof(int4) + (size_t)2 * 16 * tiles * (HD + 2) * sizeof(float));
+template <int HD, int QT>
+size_t split_bytes(int rows) {
+  return kRunGroups<HD, QT> * (sizeof(int4) + (size_t)2 * rows * (HD + 2) * sizeof(float));
+}
+
+// A step in the line.
+struct Place {
+  int env, hb, s, len, steps;
+};
+__device__ __forceinline__ Place after(const PagedAttnArgs& a, const int32_t* lens, Place p, int blocks) {
+  if (++p.s < p.steps) return p;
+  p.s = 0;
+  if (++p.hb < blocks) return p;
+  p.hb = 0;
+  do {
+    p.len = __builtin_amdgcn_readfirstlane(lens[++p.env]);
+    p.steps = steps_of(a, p.len);
+  } while (p.steps == 0);
+  return p;
 }
 
 template <int HD, CacheType T, int QT>
-__global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnArgs a, SplitSpace sp, int blocks) {
-  constexpr int NT = 64 * kSplitWaves;
-  __shared__ long long sums[kSplitWaves];
-  __shared__ long long found_base;
-  __shared__ int found_env, found_len;
+__global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, const int32_t* __restrict__ lens,
+                                                              const int32_t* __restrict__ table, SplitSpace sp, int blocks, int rows) {
+  extern __shared__ __align__(16) float lds[];
+  __shared__ long long sums[kRunWaves];
+  __shared__ int found[kRunWaves][4];                   // per wave: environment, its length, head block, step
+  __shared__ int4 ends[kRunWaves][2];                   // per wave and part: environment, head block, steps past the run, valid
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), me = blockIdx.x;
   // every workgroup adds up the steps of all environments, thread t those of a run of them
-  const int per = (a.n_env + NT - 1) / NT, e0 = min(a.n_env, tid * per), e1 = min(a.n_env, e0 + per);
+  const int per = (a.n_env + kRunThreads - 1) / kRunThreads, e0 = min(a.n_env, tid * per), e1 = min(a.n_env, e0 + per);
+  const int len0 = e0 < e1 ? lens[e0] : 0;
   long long mine = 0;
-  const int len0 = e0 < e1 ? a.lens[e0] : 0;
-  for (int e = e0; e < e1; ++e) mine += steps_of(a, e == e0 ? len0 : a.lens[e]);
+  for (int e = e0; e < e1; ++e) mine += steps_of(a, e == e0 ? len0 : lens[e]);
   long long upto = mine;
 #pragma unroll
   for (int o = 1; o < kWave; o <<= 1) {
@@ -384,76 +451,147 @@ __global__ __launch_bounds__(64 * kSplitWaves) void attn_split_kernel(PagedAttnA
     if (lane >= o) upto += v;
   }
   if (lane == 63) sums[w] = upto;
+  if (lane < 2) ends[w][lane] = make_int4(0, 0, 0, 0);
   __syncthreads();
   long long units = 0;
 #pragma unroll
-  for (int i = 0; i < kSplitWaves; ++i) {
+  for (int i = 0; i < kRunWaves; ++i) {
     if (i < w) upto += sums[i];
     units += sums[i];
   }
   units *= blocks;
-  const long long per_group = units_per_group<HD>(units), begin = min(me * per_group, units), u1 = min(begin + per_group, units);
-  long long u = begin;
-  if ((upto - mine) * blocks <= u && u < upto * blocks) {
-    long long at = (upto - mine) * blocks;
-    int e = e0, len = len0;
-    for (;;) {
-      const long long n = (long long)steps_of(a, len) * blocks;
-      if (u < at + n) break;
-      at += n;
-      len = a.lens[++e];
-    }
-    found_base = at;
-    found_env = e;
-    found_len = len;
-  }
-  int4 begun = make_int4(-1, 0, 0, 0);
-  __syncthreads();
-  if (u < u1) {
-    long long base = found_base;
-    int env = __builtin_amdgcn_readfirstlane(found_env), len = __builtin_amdgcn_readfirstlane(found_len);
-    while (u < u1) {
-      const int steps = steps_of(a, len);
-      const long long end = base + (long long)steps * blocks;
-      while (u < u1 && u < end) {
-        const int hb = __builtin_amdgcn_readfirstlane((int)((unsigned)(u - base) / (unsigned)steps));
-        const int s0 = __builtin_amdgcn_readfirstlane((int)((u - base) - (long long)hb * steps));
-        const int n = __builtin_amdgcn_readfirstlane((int)min((long long)(steps - s0), u1 - u));
-        const HeadBlock b = head_block<QT>(a, hb);
-        const int2 ids = step_pages(a, a.page_table + env * a.ld_table, s0 + w);
-        Running<HD, QT> run;
-        attend<HD, T, QT>(a, env, b, len, s0 + w, s0 + n, kSplitWaves, ids, run);
-        Partial part = {nullptr, nullptr};
-        if (n < steps) {
-          const bool began = u - s0 >= begin;
-          const size_t slot = 2 * (size_t)me + began;
-          part = {sp.o + slot * 16 * QT * HD, sp.ml + slot * 2 * 16 * QT};
-          if (began) begun = make_int4(env, hb, me + (int)((unsigned)(u - s0 + steps - 1 - begin) / (unsigned)per_group), 0);
-        }
-        __syncthreads();  // the last join's reads of LDS
-        join_waves<HD, T, QT, kSplitWaves>(a, env, b, run, part);
-        u += n;
+  constexpr unsigned kWavesAll = kRunGroups<HD, QT> * kRunWaves;
+  const long long run = max((long long)(((unsigned long long)units + kWavesAll - 1) / kWavesAll), 1ll);  // steps of a wave
+  const long long first = (upto - mine) * blocks, last = upto * blocks;  // this thread's part of the line
+#pragma unroll
+  for (int i = 0; i < kRunWaves; ++i) {
+    const long long u = ((long long)me * kRunWaves + i) * run;
+    if (first <= u && u < last) {
+      long long at = first;
+      int e = e0, len = len0;
+      for (;;) {
+        const long long n = (long long)steps_of(a, len) * blocks;
+        if (u < at + n) break;
+        at += n;
+        len = lens[++e];
       }
-      base = end;
-      if (u < u1) len = __builtin_amdgcn_readfirstlane(a.lens[++env]);
+      const unsigned steps = steps_of(a, len), r = (unsigned)(u - at), hb = r / steps;
+      found[i][0] = e;
+      found[i][1] = len;
+      found[i][2] = hb;
+      found[i][3] = r - hb * steps;
     }
+  }
+  __syncthreads();
+  const long long u0 = ((long long)me * kRunWaves + w) * run;
+  const int n = __builtin_amdgcn_readfirstlane((int)max(0ll, min(run, units - u0)));
+  Parts<HD> ps(lds, 2 * kRunWaves, rows);
+  if (n > 0) {
+    Place cur = {__builtin_amdgcn_readfirstlane(found[w][0]), __builtin_amdgcn_readfirstlane(found[w][2]),
+                 __builtin_amdgcn_readfirstlane(found[w][3]), __builtin_amdgcn_readfirstlane(found[w][1]), 0};
+    cur.steps = steps_of(a, cur.len);
+    bool began = cur.s == 0, outside;  // whether the piece began in this run
+    HeadBlock b = head_block<QT>(a, cur.hb);
+    Wave<HD, T, QT> wave(a);
+    wave.begin();
+    int2 ids = step_pages(table + cur.env * a.ld_table, a.max_pages, cur.s);
+    wave.load_q(cur.env, b);
+    ids = wave.usable(ids, cur.len, cur.s, outside);
+    wave.bad |= outside;
+    wave.load_k(ids, b.kvh);
+    wave.load_v(wave.v_at(ids, b.kvh));
+    Place next = cur;
+    if (n > 1) {
+      next = after(a, lens, cur, blocks);
+      ids = step_pages(table + next.env * a.ld_table, a.max_pages, next.s);
+    }
+    for (int i = 0; i < n; ++i) {
+      float p[QT][8];
+      wave.scores(p);
+      const bool more = i + 1 < n, ends_here = !more || next.s == 0;
+      const bf16_t* next_v = nullptr;
+      HeadBlock nb = b;
+      Place third = next;
+      if (more) {
+        if (ends_here) {
+          nb = head_block<QT>(a, next.hb);
+          wave.load_q(next.env, nb);
+        }
+        ids = wave.usable(ids, next.len, next.s, outside);
+        wave.load_k(ids, nb.kvh);
+        next_v = wave.v_at(ids, nb.kvh);
+        if (i + 2 < n) {
+          third = after(a, lens, next, blocks);
+          ids = step_pages(table + third.env * a.ld_table, a.max_pages, third.s);
+        }
+      }
+      wave.weigh(p, cur.len - kStep * cur.s);
+      if (more) wave.load_v(next_v);
+      if (ends_here) {
+        wave.end();
+        const int past = cur.steps - 1 - cur.s;  // steps of the piece after this run
+        if (began && past == 0) {
+          const int m16 = lane & 15, g = lane >> 4;
+#pragma unroll
+          for (int t = 0; t < QT; ++t)
+            if (16 * t + m16 < b.n) {
+              bf16_t* o = a.o + cur.env * a.ld_o + (size_t)(b.head0 + 16 * t + m16) * HD + 4 * g;
+              const float r = reciprocal(wave.run.l[t]);
+#pragma unroll
+              for (int j = 0; j < HD / 16; ++j) store4<T>(o + 16 * j, wave.run.o[t][j], r);
+              if (a.lse && g == 0) a.lse[(size_t)cur.env * a.n_heads + b.head0 + 16 * t + m16] = log_sum<T>(wave.run.m[t], wave.run.l[t]);
+            }
+        } else {
+          ps.put(2 * w + began, wave.run, b.n);
+          if (lane == 0) ends[w][began] = make_int4(cur.env, cur.hb, past, 1);
+        }
+        if (more) {
+          wave.begin();
+          began = true;
+        }
+      }
+      wave.bad |= more && outside;
+      cur = next;
+      next = third;
+      b = nb;
+    }
+  }
+  __syncthreads();
+  // the pieces with parts in LDS: one that began before the workgroup's run, and those that began in a wave's run
+  int4 begun = make_int4(-1, 0, 0, 0);
+  for (int w0 = -1; w0 < kRunWaves; ++w0) {
+    const bool earlier = w0 < 0;
+    int4 e = ends[earlier ? 0 : w0][earlier ? 0 : 1];
+    if (!e.w) continue;
+    const HeadBlock b = head_block<QT>(a, __builtin_amdgcn_readfirstlane(e.y));
+    const int env = __builtin_amdgcn_readfirstlane(e.x), i0 = earlier ? 0 : w0;
+    int parts = 1;
+    while (e.z > 0 && i0 + parts < kRunWaves && ends[i0 + parts][0].w) e = ends[i0 + parts++][0];  // the waves that went on
+    Partial to = {nullptr, nullptr, rows};
+    if (earlier || e.z > 0) {
+      const size_t slot = 2 * (size_t)me + !earlier;
+      to.o = sp.o + slot * rows * HD;
+      to.ml = sp.ml + slot * 2 * rows;
+      if (!earlier) begun = make_int4(env, e.y, me + 1 + (int)((unsigned)(e.z - 1) / (unsigned)(run * kRunWaves)), 0);
+    }
+    join_parts<HD, T, kRunWaves>(a, env, b, ps, earlier ? 0 : 2 * w0 + 1, parts, 2 * (i0 + 1), 2, to);
   }
   if (tid == 0) sp.begun[me] = begun;
-  for (int e = me; e < a.n_env; e += kSplitGroups<HD>) {
-    const int len = a.lens[e];
+  for (int e = me; e < a.n_env; e += kRunGroups<HD, QT>) {
+    const int len = lens[e];
     if (steps_of(a, len) == 0) no_keys<HD, T>(a, e, 0, a.n_heads, len);
   }
 }
 
-// One workgroup per (workgroup of the split, row of a head block): joins the piece that it began.
+// One workgroup per (workgroup of the run kernel, row of a head block): joins the piece that it began.
 constexpr int kJoinThreads = 256;
 template <int HD, CacheType T, int QT>
-__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp) {
+__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp, int rows) {
   constexpr int PG = kJoinThreads * 4 / HD, NW = kJoinThreads / kWave;  // PG runs of partials are added side by side
-  constexpr int PT = kSplitGroups<HD> / kJoinThreads;                   // partials per thread
-  static_assert(kSplitGroups<HD> % kJoinThreads == 0, "partials are dealt out evenly");
+  constexpr int PT = kRunGroups<HD, QT> / kJoinThreads;                 // partials per thread
+  static_assert(kRunGroups<HD, QT> % kJoinThreads == 0, "partials are dealt out evenly");
   __shared__ __align__(16) float so[PG][HD];
-  __shared__ float sc[kSplitGroups<HD>], sm[NW], sl[NW];
+  __shared__ float sc[kRunGroups<HD, QT>], sm[NW], sl[NW];
   const int w0 = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
   const int4 piece = sp.begun[w0];
   if (piece.x < 0) return;
@@ -468,9 +606,9 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
     mp[j] = -INFINITY;
     lp[j] = 0.f;
     if (i < parts) {
-      const float* ml = sp.ml + slot(i) * 2 * 16 * QT;
+      const float* ml = sp.ml + slot(i) * 2 * rows;
       mp[j] = ml[row];
-      lp[j] = ml[16 * QT + row];
+      lp[j] = ml[rows + row];
     }
     m = fmaxf(m, mp[j]);
   }
@@ -492,7 +630,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int i = pg; i < parts; i += PG) {
-    const f32x4 o = *reinterpret_cast<const f32x4*>(sp.o + slot(i) * 16 * QT * HD + row * HD + f);
+    const f32x4 o = *reinterpret_cast<const f32x4*>(sp.o + (slot(i) * rows + row) * HD + f);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], sc[i], v[e]);
   }
@@ -501,7 +639,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
   l = 0.f;
 #pragma unroll
   for (int i = 0; i < NW; ++i) l += sl[i];
-  const float r = l == 0.f ? 0.f : 1.f / l;
+  const float r = reciprocal(l);
   if (tid < HD) {
     float t = 0.f;
 #pragma unroll
@@ -512,41 +650,48 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
 }
 
 // ------------------------------------------------------------------ host
-bool split_keys(int max_pages) { return max_pages > 32; }
+int query_rows(int group, int tiles) { return std::min(16 * tiles, group); }
 
 template <int HD, CacheType T, int QT, int W>
-hipError_t launch_whole(const PagedAttnArgs& a, int blocks, hipStream_t s) {
+hipError_t launch_whole(const PagedAttnArgs& a, int blocks, int rows, hipStream_t s) {
   static LdsLimit limit;
-  constexpr size_t lds = kJoinBytes<HD, QT, W>;
-  const hipError_t e = limit.allow((const void*)attn_whole_kernel<HD, T, QT, W>, lds);
+  const hipError_t e = limit.allow((const void*)attn_whole_kernel<HD, T, QT, W>, Parts<HD>::bytes(W, 16 * QT));
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attn_whole_kernel<HD, T, QT, W>), dim3(blocks, a.n_env), dim3(64 * W), lds, s, a);
+  hipLaunchKernelGGL((attn_whole_kernel<HD, T, QT, W>), dim3(blocks, a.n_env), dim3(64 * W), Parts<HD>::bytes(W, rows), s, a, rows);
   return hipGetLastError();
 }
 
+bool split_keys(int max_pages) { static const char* e = getenv("VLA_SPLITP"); return max_pages > (e ? atoi(e) : 32); }
+
 template <int HD, CacheType T, int QT>
 hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
-  const int blocks = head_blocks<QT>(a.n_heads / a.n_kv_heads) * a.n_kv_heads;
-  if (!split_keys(a.max_pages)) return launch_whole<HD, T, QT, 4>(a, blocks, s);
+  const int group = a.n_heads / a.n_kv_heads, blocks = head_blocks<QT>(group) * a.n_kv_heads, rows = query_rows(group, QT);
+  const char* we = getenv("VLA_W");
+  const int W = we ? atoi(we) : 4;
+  if (!split_keys(a.max_pages)) {
+    if (W == 1) return launch_whole<HD, T, QT, 1>(a, blocks, rows, s);
+    if (W == 2) return launch_whole<HD, T, QT, 2>(a, blocks, rows, s);
+    if (W == 8 && QT == 1) return launch_whole<HD, T, QT, 8>(a, blocks, rows, s);
+    return launch_whole<HD, T, QT, 4>(a, blocks, rows, s);
+  }
   static LdsLimit limit;
-  constexpr size_t lds = kJoinBytes<HD, QT, kSplitWaves>;
-  const hipError_t e = limit.allow((const void*)attn_split_kernel<HD, T, QT>, lds);
+  const hipError_t e = limit.allow((const void*)attn_run_kernel<HD, T, QT>, Parts<HD>::bytes(2 * kRunWaves, 16 * QT));
   if (e != hipSuccess) return e;
-  const SplitSpace sp = split_space<HD, QT>(a.ws);
-  const int rows = std::min(16 * QT, a.n_heads / a.n_kv_heads);
-  hipLaunchKernelGGL((attn_split_kernel<HD, T, QT>), dim3(kSplitGroups<HD>), dim3(64 * kSplitWaves), lds, s, a, sp, blocks);
-  hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(kSplitGroups<HD>, rows), dim3(kJoinThreads), 0, s, a, sp);
+  const SplitSpace sp = split_space<HD, QT>(a.ws, rows);
+  hipLaunchKernelGGL((attn_run_kernel<HD, T, QT>), dim3(kRunGroups<HD, QT>), dim3(kRunThreads),
+                     Parts<HD>::bytes(2 * kRunWaves, rows), s, a, a.lens, a.page_table, sp, blocks, rows);
+  hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(kRunGroups<HD, QT>, rows), dim3(kJoinThreads), 0, s, a, sp, rows);
   return hipGetLastError();
 }
 
 // Query heads of a group by tiles of 16: up to head_dim 128 two share a step's keys in registers (at 256 two tiles' sums do
 // not fit), further ones read the keys again.
-int query_tiles(int n_heads, int n_kv_heads, int head_dim) { return head_dim < 256 && n_heads / n_kv_heads > 16 ? 2 : 1; }
+int query_tiles(int group, int head_dim) { return head_dim < 256 && group > 16 ? 2 : 1; }
 
 template <int HD, CacheType T>
 hipError_t launch_heads(const PagedAttnArgs& a, hipStream_t s) {
   if constexpr (HD < 256)
-    if (query_tiles(a.n_heads, a.n_kv_heads, HD) == 2) return launch_blocks<HD, T, 2>(a, s);
+    if (query_tiles(a.n_heads / a.n_kv_heads, HD) == 2) return launch_blocks<HD, T, 2>(a, s);
   return launch_blocks<HD, T, 1>(a, s);
 }
 template <CacheType T>
@@ -561,8 +706,10 @@ hipError_t launch_type(const PagedAttnArgs& a, hipStream_t s) {
 
 size_t paged_attn_bytes(int, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
   if (!split_keys(max_pages)) return 256;
-  const int tiles = query_tiles(n_heads, n_kv_heads, head_dim);
-  return head_dim == 64 ? split_bytes<64>(tiles) : head_dim == 128 ? split_bytes<128>(tiles) : split_bytes<256>(tiles);
+  const int group = n_heads / n_kv_heads, tiles = query_tiles(group, head_dim), rows = query_rows(group, tiles);
+  if (head_dim == 64) return tiles == 1 ? split_bytes<64, 1>(rows) : split_bytes<64, 2>(rows);
+  if (head_dim == 128) return tiles == 1 ? split_bytes<128, 1>(rows) : split_bytes<128, 2>(rows);
+  return split_bytes<256, 1>(rows);
 }
 
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s) {
