@@ -203,8 +203,9 @@ static int check_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, i
   if (n_heads % n_kv_heads != 0) return set_error(VLA_EINVAL, "n_heads must be a multiple of n_kv_heads");
   if (n_env > 65535 || max_pages >= 1 << 26)
     return set_error(VLA_EUNSUPPORTED, "at most 65535 environments and 2^26 - 1 pages of one");
-  if ((int64_t)max_pages * n_heads >= (int64_t)1 << 31 || (double)n_env * max_pages * n_heads >= 0x1p40)
-    return set_error(VLA_EUNSUPPORTED, "max_pages * n_heads must be below 2^31, and below 2^40 over all environments");
+  if ((int64_t)max_pages * n_heads >= (int64_t)1 << 31 || (int64_t)max_pages * n_env >= (int64_t)1 << 31 ||
+      (double)n_env * max_pages * n_heads >= 0x1p40)
+    return set_error(VLA_EUNSUPPORTED, "max_pages * n_heads and max_pages * n_env must be below 2^31, all three below 2^40");
   return VLA_OK;
 }
 

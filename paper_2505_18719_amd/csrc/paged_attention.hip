@@ -10,8 +10,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
-#include <type_traits>
 
 #include "cache.h"
 #include "common.h"
@@ -22,9 +20,6 @@ namespace {
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
-#ifndef GROUPSX
-#define GROUPSX (HD == 256 || (HD == 128 && QT == 2) ? 256 : HD == 64 && QT == 1 ? 1024 : 512)
-#endif
 constexpr int kStep = 32;  // keys of a wave's step
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
@@ -109,13 +104,11 @@ struct Running {
   f32x4 o[QT][HD / 16];
 };
 
-typedef unsigned u32x4v __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ uint4 load_once(const bf16_t* p) {  // past the caches: a page is read by one wave
-  #ifdef PLAINX
-  const u32x4v v = *reinterpret_cast<const u32x4v*>(p);
-#else
-  const u32x4v v = __builtin_nontemporal_load(reinterpret_cast<const u32x4v*>(p));
-#endif
+// 16 bytes of a page: past the caches where the pool is larger than they keep (STREAM).
+template <bool STREAM>
+__device__ __forceinline__ uint4 load_page(const bf16_t* p) {
+  const u32x4* src = reinterpret_cast<const u32x4*>(p);
+  const u32x4 v = STREAM ? __builtin_nontemporal_load(src) : *src;
   return make_uint4(v.x, v.y, v.z, v.w);
 }
 
@@ -125,7 +118,7 @@ __device__ __forceinline__ int2 step_pages(const int32_t* pt, int max_pages, int
 }
 
 // A wave at its steps.
-template <int HD, CacheType T, int QT>
+template <int HD, CacheType T, int QT, bool STREAM>
 struct Wave {
   static constexpr int KC = HD / 32, VC = HD / 16;
   const PagedAttnArgs& a;
@@ -172,14 +165,14 @@ struct Wave {
 #pragma unroll
     for (int i = 0; i < KC; ++i)
 #pragma unroll
-      for (int t = 0; t < 2; ++t) k[t][i] = load_once(p + 4 * t * HD + 32 * i);
+      for (int t = 0; t < 2; ++t) k[t][i] = load_page<STREAM>(p + 4 * t * HD + 32 * i);
   }
   __device__ __forceinline__ const bf16_t* v_at(int2 ids, int kvh) const {
     return a.pages.v + ((size_t)kvh * HD + m16) * kPage + 8 * (g & 1) + (g < 2 ? ids.x : ids.y) * page_elems;
   }
   __device__ __forceinline__ void load_v(const bf16_t* p) {
 #pragma unroll
-    for (int i = 0; i < VC; ++i) v[i] = load_once(p + 16 * i * kPage);
+    for (int i = 0; i < VC; ++i) v[i] = load_page<STREAM>(p + 16 * i * kPage);
   }
 
   // p = base-2 scores of the step's keys; k and q are free afterwards
@@ -345,7 +338,7 @@ __device__ __forceinline__ void no_keys(const PagedAttnArgs& a, int env, int hea
 }
 
 // One workgroup of W waves per (head block, environment); wave w takes steps w, w + W, ...
-template <int HD, CacheType T, int QT, int W>
+template <int HD, CacheType T, int QT, bool STREAM, int W>
 __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a, int rows) {
   extern __shared__ __align__(16) float lds[];
   const int env = blockIdx.y, len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
@@ -354,7 +347,7 @@ __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a, int
   const int32_t* pt = a.page_table + env * a.ld_table;
   int2 ids = a.max_pages > 0 ? step_pages(pt, a.max_pages, w) : make_int2(0, 0);
   if (steps == 0) return no_keys<HD, T>(a, env, b.head0, b.n, len);
-  Wave<HD, T, QT> wave(a);
+  Wave<HD, T, QT, STREAM> wave(a);
   wave.begin();
   if (w < steps) {
     bool outside;
@@ -395,9 +388,10 @@ __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a, int
 // the run's ends is left in LDS, joined there with the neighbouring waves' parts, and what runs past the workgroup's ends
 // goes to the workspace: slot 2 w + 1 of workgroup w if the piece began there, else 2 w.  Who began a piece notes it down
 // for attn_join_kernel, which adds its partials in order.
+// Workgroups that the registers leave room for at once (64 x 4096 keys, 16 heads of 64: 254 us with 512, 174 with 1024).
 template <int HD, int QT>
-constexpr int kRunGroups = GROUPSX;
-constexpr int kRunWaves = 4, kRunThreads = 64 * kRunWaves;
+constexpr int kRunGroups = HD == 256 || (HD == 128 && QT == 2) ? 256 : HD == 64 && QT == 1 ? 1024 : 512;
+constexpr int kRunWaves = 4, kRunThreads = 64 * kRunWaves;  // the grid may be smaller than kRunGroups where the lengths cannot need it
 
 struct SplitSpace {
   int4* begun;  // [groups] the piece that workgroup w began and did not end: environment, head block, last workgroup; or -1
@@ -413,6 +407,17 @@ SplitSpace split_space(void* ws, int rows) {
 template <int HD, int QT>
 size_t split_bytes(int rows) {
   return kRunGroups<HD, QT> * (sizeof(int4) + (size_t)2 * rows * (HD + 2) * sizeof(float));
+}
+
+// Sum over this lane and those before it.
+__device__ __forceinline__ int wave_scan(int v) {
+  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // the lane 1, 2, 4, 8 before in its 16
+  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 to the second 16 (47 to the fourth)
+  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to the second 32
+  return v;
 }
 
 // A step in the line.
@@ -431,68 +436,50 @@ __device__ __forceinline__ Place after(const PagedAttnArgs& a, const int32_t* le
   return p;
 }
 
-template <int HD, CacheType T, int QT>
+template <int HD, CacheType T, int QT, bool STREAM>
 __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, const int32_t* __restrict__ lens,
                                                               const int32_t* __restrict__ table, SplitSpace sp, int blocks, int rows) {
   extern __shared__ __align__(16) float lds[];
-  __shared__ long long sums[kRunWaves];
-  __shared__ int found[kRunWaves][4];                   // per wave: environment, its length, head block, step
-  __shared__ int4 ends[kRunWaves][2];                   // per wave and part: environment, head block, steps past the run, valid
+  __shared__ int4 ends[kRunWaves][2];  // per wave and part: environment, head block, steps past the run, valid
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), me = blockIdx.x;
-  // every workgroup adds up the steps of all environments, thread t those of a run of them
-  const int per = (a.n_env + kRunThreads - 1) / kRunThreads, e0 = min(a.n_env, tid * per), e1 = min(a.n_env, e0 + per);
-  const int len0 = e0 < e1 ? lens[e0] : 0;
-  long long mine = 0;
-  for (int e = e0; e < e1; ++e) mine += steps_of(a, e == e0 ? len0 : lens[e]);
-  long long upto = mine;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const long long v = __shfl_up(upto, o, kWave);
-    if (lane >= o) upto += v;
-  }
-  if (lane == 63) sums[w] = upto;
   if (lane < 2) ends[w][lane] = make_int4(0, 0, 0, 0);
-  __syncthreads();
-  long long units = 0;
-#pragma unroll
-  for (int i = 0; i < kRunWaves; ++i) {
-    if (i < w) upto += sums[i];
-    units += sums[i];
+  // every wave adds up the steps of all environments, each lane those of a run of them, and finds its place in the line
+  const int per = (a.n_env + kWave - 1) / kWave, e0 = min(a.n_env, lane * per), e1 = min(a.n_env, e0 + per);
+  const int len0 = e0 < e1 ? lens[e0] : 0;
+  int mine = 0;
+  bool empty = false;  // an environment without steps
+  for (int e = e0; e < e1; ++e) {
+    const int n = steps_of(a, e == e0 ? len0 : lens[e]);
+    mine += n;
+    empty |= n == 0;
   }
-  units *= blocks;
+  const int upto = wave_scan(mine);
+  const long long units = (long long)__builtin_amdgcn_readlane(upto, kWave - 1) * blocks;
   constexpr unsigned kWavesAll = kRunGroups<HD, QT> * kRunWaves;
   const long long run = max((long long)(((unsigned long long)units + kWavesAll - 1) / kWavesAll), 1ll);  // steps of a wave
-  const long long first = (upto - mine) * blocks, last = upto * blocks;  // this thread's part of the line
-#pragma unroll
-  for (int i = 0; i < kRunWaves; ++i) {
-    const long long u = ((long long)me * kRunWaves + i) * run;
-    if (first <= u && u < last) {
-      long long at = first;
-      int e = e0, len = len0;
-      for (;;) {
-        const long long n = (long long)steps_of(a, len) * blocks;
-        if (u < at + n) break;
-        at += n;
-        len = lens[++e];
-      }
-      const unsigned steps = steps_of(a, len), r = (unsigned)(u - at), hb = r / steps;
-      found[i][0] = e;
-      found[i][1] = len;
-      found[i][2] = hb;
-      found[i][3] = r - hb * steps;
-    }
-  }
-  __syncthreads();
-  const long long u0 = ((long long)me * kRunWaves + w) * run;
+  const long long u0 = ((long long)me * kRunWaves + w) * run, first = (long long)(upto - mine) * blocks;
   const int n = __builtin_amdgcn_readfirstlane((int)max(0ll, min(run, units - u0)));
+  int e = e0, len = len0;
+  long long at = first;
+  const bool here = first <= u0 && u0 < (long long)upto * blocks;
+  if (here)
+    for (;;) {
+      const long long m = (long long)steps_of(a, len) * blocks;
+      if (u0 < at + m) break;
+      at += m;
+      len = lens[++e];
+    }
+  const int holder = n > 0 ? __builtin_ctzll(__ballot(here)) : 0;
+  const int env0 = __builtin_amdgcn_readlane(e, holder), len_0 = __builtin_amdgcn_readlane(len, holder);
+  const unsigned into = __builtin_amdgcn_readlane((int)(u0 - at), holder);  // steps from the environment's first to u0
   Parts<HD> ps(lds, 2 * kRunWaves, rows);
   if (n > 0) {
-    Place cur = {__builtin_amdgcn_readfirstlane(found[w][0]), __builtin_amdgcn_readfirstlane(found[w][2]),
-                 __builtin_amdgcn_readfirstlane(found[w][3]), __builtin_amdgcn_readfirstlane(found[w][1]), 0};
-    cur.steps = steps_of(a, cur.len);
+    Place cur = {env0, 0, 0, len_0, steps_of(a, len_0)};
+    cur.hb = into / (unsigned)cur.steps;
+    cur.s = into - cur.hb * cur.steps;
     bool began = cur.s == 0, outside;  // whether the piece began in this run
     HeadBlock b = head_block<QT>(a, cur.hb);
-    Wave<HD, T, QT> wave(a);
+    Wave<HD, T, QT, STREAM> wave(a);
     wave.begin();
     int2 ids = step_pages(table + cur.env * a.ld_table, a.max_pages, cur.s);
     wave.load_q(cur.env, b);
@@ -558,26 +545,38 @@ __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, 
   }
   __syncthreads();
   // the pieces with parts in LDS: one that began before the workgroup's run, and those that began in a wave's run
-  int4 begun = make_int4(-1, 0, 0, 0);
+  int4 head[kRunWaves], tail[kRunWaves], begun = make_int4(-1, 0, 0, 0);
+#pragma unroll
+  for (int i = 0; i < kRunWaves; ++i) {
+    head[i] = ends[i][0];
+    tail[i] = ends[i][1];
+  }
+#pragma unroll
   for (int w0 = -1; w0 < kRunWaves; ++w0) {
     const bool earlier = w0 < 0;
-    int4 e = ends[earlier ? 0 : w0][earlier ? 0 : 1];
-    if (!e.w) continue;
-    const HeadBlock b = head_block<QT>(a, __builtin_amdgcn_readfirstlane(e.y));
-    const int env = __builtin_amdgcn_readfirstlane(e.x), i0 = earlier ? 0 : w0;
+    int4 end = earlier ? head[0] : tail[max(w0, 0)];
+    if (!__builtin_amdgcn_readfirstlane(end.w)) continue;
+    const HeadBlock b = head_block<QT>(a, __builtin_amdgcn_readfirstlane(end.y));
+    const int env = __builtin_amdgcn_readfirstlane(end.x), i0 = max(w0, 0);
     int parts = 1;
-    while (e.z > 0 && i0 + parts < kRunWaves && ends[i0 + parts][0].w) e = ends[i0 + parts++][0];  // the waves that went on
+#pragma unroll
+    for (int i = i0 + 1; i < kRunWaves; ++i)  // the waves that went on
+      if (parts == i - i0 && end.z > 0 && head[i].w) {
+        end = head[i];
+        ++parts;
+      }
     Partial to = {nullptr, nullptr, rows};
-    if (earlier || e.z > 0) {
+    if (earlier || end.z > 0) {
       const size_t slot = 2 * (size_t)me + !earlier;
       to.o = sp.o + slot * rows * HD;
       to.ml = sp.ml + slot * 2 * rows;
-      if (!earlier) begun = make_int4(env, e.y, me + 1 + (int)((unsigned)(e.z - 1) / (unsigned)(run * kRunWaves)), 0);
+      if (!earlier) begun = make_int4(env, end.y, me + 1 + (int)((unsigned)(end.z - 1) / (unsigned)(run * kRunWaves)), 0);
     }
-    join_parts<HD, T, kRunWaves>(a, env, b, ps, earlier ? 0 : 2 * w0 + 1, parts, 2 * (i0 + 1), 2, to);
+    join_parts<HD, T, kRunWaves>(a, env, b, ps, earlier ? 0 : 2 * w0 + 1, __builtin_amdgcn_readfirstlane(parts), 2 * (i0 + 1), 2, to);
   }
   if (tid == 0) sp.begun[me] = begun;
-  for (int e = me; e < a.n_env; e += kRunGroups<HD, QT>) {
+  if (!__any(empty)) return;
+  for (int e = me; e < a.n_env; e += gridDim.x) {
     const int len = lens[e];
     if (steps_of(a, len) == 0) no_keys<HD, T>(a, e, 0, a.n_heads, len);
   }
@@ -652,47 +651,66 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
 // ------------------------------------------------------------------ host
 int query_rows(int group, int tiles) { return std::min(16 * tiles, group); }
 
-template <int HD, CacheType T, int QT, int W>
+template <int HD, CacheType T, int QT, bool STREAM, int W>
 hipError_t launch_whole(const PagedAttnArgs& a, int blocks, int rows, hipStream_t s) {
   static LdsLimit limit;
-  const hipError_t e = limit.allow((const void*)attn_whole_kernel<HD, T, QT, W>, Parts<HD>::bytes(W, 16 * QT));
+  const auto kernel = attn_whole_kernel<HD, T, QT, STREAM, W>;
+  const hipError_t e = limit.allow((const void*)kernel, Parts<HD>::bytes(W, 16 * QT));
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((attn_whole_kernel<HD, T, QT, W>), dim3(blocks, a.n_env), dim3(64 * W), Parts<HD>::bytes(W, rows), s, a, rows);
+  hipLaunchKernelGGL(kernel, dim3(blocks, a.n_env), dim3(64 * W), Parts<HD>::bytes(W, rows), s, a, rows);
   return hipGetLastError();
 }
 
-bool split_keys(int max_pages) { static const char* e = getenv("VLA_SPLITP"); return max_pages > (e ? atoi(e) : 32); }
-
-template <int HD, CacheType T, int QT>
-hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
-  const int group = a.n_heads / a.n_kv_heads, blocks = head_blocks<QT>(group) * a.n_kv_heads, rows = query_rows(group, QT);
-  const char* we = getenv("VLA_W");
-  const int W = we ? atoi(we) : 4;
-  if (!split_keys(a.max_pages)) {
-    if (W == 1) return launch_whole<HD, T, QT, 1>(a, blocks, rows, s);
-    if (W == 2) return launch_whole<HD, T, QT, 2>(a, blocks, rows, s);
-    if (W == 8 && QT == 1) return launch_whole<HD, T, QT, 8>(a, blocks, rows, s);
-    return launch_whole<HD, T, QT, 4>(a, blocks, rows, s);
-  }
+template <int HD, CacheType T, int QT, bool STREAM>
+hipError_t launch_run(const PagedAttnArgs& a, int blocks, int rows, hipStream_t s) {
   static LdsLimit limit;
-  const hipError_t e = limit.allow((const void*)attn_run_kernel<HD, T, QT>, Parts<HD>::bytes(2 * kRunWaves, 16 * QT));
+  const auto kernel = attn_run_kernel<HD, T, QT, STREAM>;
+  const hipError_t e = limit.allow((const void*)kernel, Parts<HD>::bytes(2 * kRunWaves, 16 * QT));
   if (e != hipSuccess) return e;
   const SplitSpace sp = split_space<HD, QT>(a.ws, rows);
-  hipLaunchKernelGGL((attn_run_kernel<HD, T, QT>), dim3(kRunGroups<HD, QT>), dim3(kRunThreads),
-                     Parts<HD>::bytes(2 * kRunWaves, rows), s, a, a.lens, a.page_table, sp, blocks, rows);
-  hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(kRunGroups<HD, QT>, rows), dim3(kJoinThreads), 0, s, a, sp, rows);
+  const long long most = (long long)a.n_env * blocks * ((a.max_pages + 1) / 2);  // steps of full lengths
+  const int groups = (int)std::min((long long)kRunGroups<HD, QT>, (most + kRunWaves - 1) / kRunWaves);
+  hipLaunchKernelGGL(kernel, dim3(groups), dim3(kRunThreads), Parts<HD>::bytes(2 * kRunWaves, rows), s, a, a.lens, a.page_table, sp,
+                     blocks, rows);
+  hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(groups, rows), dim3(kJoinThreads), 0, s, a, sp, rows);
   return hipGetLastError();
+}
+
+// Up to 512 tokens the two launches of the split cost more than they save, whatever the number of items (GPU us, whole /
+// split: 278 tokens, 32 key heads 7.6 / 10.3; 512 tokens, 8 key heads 9.4 / 9.6; 64 x 300, 8 key heads 16 / 25); beyond, the
+// split is as fast where items abound and faster where they are few or uneven (1024 tokens, 8 key heads 16.9 / 9.8; 64 of
+// up to 2048 56 / 54).
+bool split_keys(int max_pages) { return max_pages > 32; }
+
+template <int HD, CacheType T, int QT, bool STREAM>
+hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
+  const int group = a.n_heads / a.n_kv_heads, blocks = head_blocks<QT>(group) * a.n_kv_heads, rows = query_rows(group, QT);
+  if (split_keys(a.max_pages)) return launch_run<HD, T, QT, STREAM>(a, blocks, rows, s);
+  // One wave per item where those fill the GPU, else four (us, one / four: 512 x 30 tokens, 8 key heads 16 / 28; 512 x 128
+  // 47 / 53; 64 x 300, 32 key heads 52.9 / 54; 512 items of 300 tokens 16.9 / 16.2, 256 of 64 5.2 / 4.7)
+  if ((long long)blocks * a.n_env >= 1024) return launch_whole<HD, T, QT, STREAM, 1>(a, blocks, rows, s);
+  return launch_whole<HD, T, QT, STREAM, 4>(a, blocks, rows, s);
 }
 
 // Query heads of a group by tiles of 16: up to head_dim 128 two share a step's keys in registers (at 256 two tiles' sums do
 // not fit), further ones read the keys again.
 int query_tiles(int group, int head_dim) { return head_dim < 256 && group > 16 ? 2 : 1; }
 
+// A pool of up to 32 MB, the L2s' size, may be in the caches from one step to the next (278 tokens, 32 key heads: 6.2 us with
+// cached loads, 7.5 past the caches); beyond, reads past the caches are faster (64 x 4096: 191 and 173 us).
+bool stream_pool(const PagedAttnArgs& a) {
+  return (size_t)a.n_pages * a.n_kv_heads * kPage * a.head_dim * 2 * sizeof(bf16_t) > (size_t)32 << 20;
+}
+
+template <int HD, CacheType T, int QT>
+hipError_t launch_tiles(const PagedAttnArgs& a, hipStream_t s) {
+  return stream_pool(a) ? launch_blocks<HD, T, QT, true>(a, s) : launch_blocks<HD, T, QT, false>(a, s);
+}
 template <int HD, CacheType T>
 hipError_t launch_heads(const PagedAttnArgs& a, hipStream_t s) {
   if constexpr (HD < 256)
-    if (query_tiles(a.n_heads / a.n_kv_heads, HD) == 2) return launch_blocks<HD, T, 2>(a, s);
-  return launch_blocks<HD, T, 1>(a, s);
+    if (query_tiles(a.n_heads / a.n_kv_heads, HD) == 2) return launch_tiles<HD, T, 2>(a, s);
+  return launch_tiles<HD, T, 1>(a, s);
 }
 template <CacheType T>
 hipError_t launch_type(const PagedAttnArgs& a, hipStream_t s) {
