@@ -504,58 +504,68 @@ ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
 ROPE_SCALINGS = ("none", "linear", "base", "bands", "ramp")
 
 
-class _on:
-    """Makes `device` current for a launch on its stream, where it is not."""
-
-    __slots__ = ("guard",)
-
-    def __init__(self, device):
-        self.guard = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-
-    def __enter__(self):
-        if self.guard is not None:
-            self.guard.__enter__()
-
-    def __exit__(self, *exc):
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+# The address of the current stream of a device by its index (a tenth of the time of torch.cuda.current_stream, which
+# counts in a decode step: these calls' GPU work is a few microseconds)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _at(t: Optional[torch.Tensor], dtype, device, name: str, shape=None):
-    """Address of a contiguous tensor of `dtype` on `device` (None stays None)."""
+def _launch(index: int, fn, *args) -> None:
+    """fn(*args, current stream of device `index`) with that device current."""
+    if torch.cuda.current_device() == index:
+        code = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            code = fn(*args, _raw_stream(index))
+    if code != VLA_OK:
+        _check(code)
+
+
+def _at(t: Optional[torch.Tensor], dtype, index: int, name: str, *shape):
+    """Address of a contiguous tensor of `dtype` and `shape` on device `index` (None stays None)."""
     if t is None:
         return None
-    if t.dtype != dtype or t.device != device or not t.is_contiguous() or (shape is not None and t.shape != shape):
-        raise ValueError(f"{name} must be a contiguous {dtype} tensor on {device}"
-                         + (f" of shape {tuple(shape)}" if shape is not None else ""))
+    if t.dtype is not dtype or t.get_device() != index or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"{name} must be a contiguous {dtype} tensor of shape {shape} on device {index}")
     return t.data_ptr() or None
 
 
-def _head_rows(t: torch.Tensor, like: torch.Tensor, name: str, heads: Optional[int] = None):
+def _head_rows(t: torch.Tensor, dtype, index: int, name: str, rows: int, heads: int, head_dim: int):
     """Address and row stride of [rows, heads, head_dim] whose rows hold their heads contiguously."""
-    if t.dim() != 3 or t.dtype != like.dtype or t.device != like.device or t.shape[0] != like.shape[0] \
-            or t.shape[2] != like.shape[2] or (heads is not None and t.shape[1] != heads):
-        raise ValueError(f"{name} must be [rows, heads, head_dim] with the rows, head_dim, type and device of q")
-    n, h, d = t.shape
+    if t.dtype is not dtype or t.get_device() != index or t.shape != (rows, heads, head_dim):
+        raise ValueError(f"{name} must be a {dtype} tensor of shape {(rows, heads, head_dim)} on device {index}")
     sr, sh, sd = t.stride()
-    if sd != 1 or (h > 1 and sh != d):
+    if sd != 1 or (sh != head_dim and heads > 1):
         raise ValueError(f"{name} must hold the heads of a row contiguously")
-    return t.data_ptr() or None, (sr if n > 1 else h * d)
+    return t.data_ptr() or None, (sr if rows > 1 else heads * head_dim)
 
 
-def _cache_dtype(t: torch.Tensor) -> int:
-    if not t.is_cuda or t.dtype not in CACHE_DTYPES:
-        raise ValueError("expected bfloat16 or float16 device tensors")
-    return CACHE_DTYPES[t.dtype]
+def _heads(t: torch.Tensor, name: str):
+    """(rows, heads, head_dim, dtype number, device index) of a [rows, heads, head_dim] device tensor."""
+    dt, index = CACHE_DTYPES.get(t.dtype), t.get_device()
+    if dt is None or index < 0 or t.dim() != 3:
+        raise ValueError(f"{name} must be a bfloat16 or float16 device tensor [rows, heads, head_dim]")
+    return (*t.shape, dt, index)
 
 
-def _pages(k_pages: torch.Tensor, v_pages: torch.Tensor, like: torch.Tensor, kv_heads: Optional[int] = None):
-    """Addresses of the pools, their number of pages and key heads."""
-    n, h, d = k_pages.shape[0], k_pages.shape[1], like.shape[2]
-    if k_pages.dim() != 4 or kv_heads not in (None, h):
-        raise ValueError("k_pages must be [n_pages, n_kv_heads, 16, head_dim]")
-    return (_at(k_pages, like.dtype, like.device, "k_pages", (n, h, CACHE_PAGE, d)),
-            _at(v_pages, like.dtype, like.device, "v_pages", (n, h, d, CACHE_PAGE)), n, h)
+def _pool(k_pages: torch.Tensor, v_pages: Optional[torch.Tensor], dtype, index: int, head_dim: int):
+    """Addresses of a cache's pages, their number and their key heads."""
+    if k_pages.dim() != 4 or v_pages is None:
+        raise ValueError("k_pages must be [n_pages, n_kv_heads, 16, head_dim] and come with v_pages")
+    n, h = k_pages.shape[:2]
+    return (_at(k_pages, dtype, index, "k_pages", n, h, CACHE_PAGE, head_dim),
+            _at(v_pages, dtype, index, "v_pages", n, h, head_dim, CACHE_PAGE), n, h)
+
+
+def _table(t: torch.Tensor, index: int, n_env: int):
+    """Address, row stride and columns of an int32 page table [n_env, max_pages] with contiguous rows."""
+    if t.dtype is not torch.int32 or t.get_device() != index or t.dim() != 2 or t.shape[0] != n_env:
+        raise ValueError(f"page_table must be an int32 tensor [{n_env}, max_pages] on device {index}")
+    cols = t.shape[1]
+    ld, inner = t.stride()
+    if n_env > 0 and cols > 1 and inner != 1:
+        raise ValueError("page_table must have contiguous rows")
+    return t.data_ptr() or None, (ld if n_env > 1 else cols), cols
 
 
 def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
@@ -574,27 +584,20 @@ def kv_plan(cached_lens: torch.Tensor, new_lens: torch.Tensor, page_table: torch
             out: Optional[Dict[str, torch.Tensor]] = None) -> Dict[str, torch.Tensor]:
     """New pages (into page_table) and the new tokens' rows of a step (vla_kv_plan): {lens [n_env], row_start [n_env + 1],
     row_pos, row_env, row_slot [max_rows], stats [3]: free_head after, rows, refused}, all int32."""
-    lib = load_library()
-    dev, i32 = cached_lens.device, torch.int32
-    if not cached_lens.is_cuda or cached_lens.dim() != 1 or page_table.dim() != 2 or free_pages.dim() != 1:
-        raise ValueError("cached_lens [n_env], page_table [n_env, max_pages] and free_pages [n_free] must be device tensors")
-    n, (rows_t, max_pages) = cached_lens.shape[0], page_table.shape
-    if page_table.dtype != i32 or page_table.device != dev or rows_t != n \
-            or (n > 0 and max_pages > 1 and page_table.stride(1) != 1):
-        raise ValueError("page_table must be int32 [n_env, max_pages] with contiguous rows")
+    lib = _lib or load_library()
+    i32, index = torch.int32, cached_lens.get_device()
+    if index < 0 or cached_lens.dim() != 1 or free_pages.dim() != 1:
+        raise ValueError("cached_lens [n_env] and free_pages [n_free] must be device tensors")
+    n, n_free = cached_lens.shape[0], free_pages.shape[0]
+    table, ld, max_pages = _table(page_table, index, n)
+    names, sizes = ("lens", "row_start", "row_pos", "row_env", "row_slot", "stats"), (n, n + 1, max_rows, max_rows, max_rows, 3)
     if out is None:
-        buf = torch.empty(2 * n + 1 + 3 * max_rows + 3, dtype=i32, device=dev)
-        parts = buf.split([n, n + 1, max_rows, max_rows, max_rows, 3])
-        out = dict(zip(("lens", "row_start", "row_pos", "row_env", "row_slot", "stats"), parts))
-    ld = page_table.stride(0) if n > 1 else max_pages
-    with _on(dev):
-        _check(lib.vla_kv_plan(
-            n, _at(cached_lens, i32, dev, "cached_lens"), _at(new_lens, i32, dev, "new_lens", (n,)),
-            page_table.data_ptr() or None, ld, max_pages, _at(free_pages, i32, dev, "free_pages"), free_pages.shape[0],
-            _at(free_head, i32, dev, "free_head", (1,)), n_pages, max_rows, _at(out["lens"], i32, dev, "lens", (n,)),
-            _at(out["row_start"], i32, dev, "row_start", (n + 1,)), _at(out["row_pos"], i32, dev, "row_pos", (max_rows,)),
-            _at(out["row_env"], i32, dev, "row_env", (max_rows,)), _at(out["row_slot"], i32, dev, "row_slot", (max_rows,)),
-            _at(out["stats"], i32, dev, "stats", (3,)), torch.cuda.current_stream(dev).cuda_stream))
+        buf = torch.empty(sum(sizes), dtype=i32, device=cached_lens.device)
+        out = dict(zip(names, buf.split_with_sizes(sizes)))
+    _launch(index, lib.vla_kv_plan, n, _at(cached_lens, i32, index, "cached_lens", n),
+            _at(new_lens, i32, index, "new_lens", n), table, ld, max_pages, _at(free_pages, i32, index, "free_pages", n_free),
+            n_free, _at(free_head, i32, index, "free_head", 1), n_pages, max_rows,
+            *[_at(out[k], i32, index, k, s) for k, s in zip(names, sizes)])
     return out
 
 
@@ -607,30 +610,32 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, row_pos: Optional[torch.Tenso
     """Head norms and rotation of q [rows, n_heads, head_dim] and k [rows, n_kv_heads, head_dim] (views of one projection's
     output will do), and with pages the append of k and v at row_slot (vla_qk_norm_rope).  Returns (q_out, k_out); with a
     cache k_out is written only if it is passed in."""
-    lib = load_library()
-    dt, dev = _cache_dtype(q), q.device
-    rows, H, hd = q.shape
-    K = k.shape[1]
-    cache = k_pages is not None
+    lib = _lib or load_library()
+    rows, H, hd, dt, index = _heads(q, "q")
+    dtype, K = q.dtype, k.shape[1]
     if q_out is None:
-        q_out = torch.empty((rows, H, hd), dtype=q.dtype, device=dev)
-    if k_out is None and not cache:
-        k_out = torch.empty((rows, K, hd), dtype=q.dtype, device=dev)
-    rot = 0 if freqs is None else 2 * freqs.numel()
-    qp, qs = _head_rows(q, q, "q")
-    kp, ks = _head_rows(k, q, "k", K)
-    vp, vs = (None, 0) if v is None else _head_rows(v, q, "v", K)
-    qo, qos = _head_rows(q_out, q, "q_out", H)
-    ko, kos = (None, 0) if k_out is None else _head_rows(k_out, q, "k_out", K)
-    pk, pv, n_pages = _pages(k_pages, v_pages, q, K)[:3] if cache else (None, None, 0)
+        q_out = torch.empty((rows, H, hd), dtype=dtype, device=q.device)
+    if k_out is None and k_pages is None:
+        k_out = torch.empty((rows, K, hd), dtype=dtype, device=q.device)
+    qp, qs = _head_rows(q, dtype, index, "q", rows, H, hd)
+    kp, ks = _head_rows(k, dtype, index, "k", rows, K, hd)
+    vp, vs = (None, 0) if v is None else _head_rows(v, dtype, index, "v", rows, K, hd)
+    qo, qos = _head_rows(q_out, dtype, index, "q_out", rows, H, hd)
+    ko, kos = (None, 0) if k_out is None else _head_rows(k_out, dtype, index, "k_out", rows, K, hd)
+    pk = pv = None
+    n_pages = rot = 0
+    if k_pages is not None:
+        pk, pv, n_pages, kv = _pool(k_pages, v_pages, dtype, index, hd)
+        if kv != K:
+            raise ValueError("the pages must have the heads of k")
+    if freqs is not None:
+        rot = 2 * freqs.shape[0]
     if rows == 0:
         return q_out, k_out
-    with _on(dev):
-        _check(lib.vla_qk_norm_rope(
-            rows, H, K, hd, dt, qp, qs, kp, ks, vp, vs, _at(q_gain, q.dtype, dev, "q_gain", (hd,)),
-            _at(k_gain, q.dtype, dev, "k_gain", (hd,)), eps, _at(row_pos, torch.int32, dev, "row_pos", (rows,)),
-            _at(freqs, torch.float64, dev, "freqs"), rot, ROPE_LAYOUTS[layout], rope_scale, qo, qos, ko, kos, pk, pv,
-            n_pages, _at(row_slot, torch.int32, dev, "row_slot", (rows,)), torch.cuda.current_stream(dev).cuda_stream))
+    _launch(index, lib.vla_qk_norm_rope, rows, H, K, hd, dt, qp, qs, kp, ks, vp, vs, _at(q_gain, dtype, index, "q_gain", hd),
+            _at(k_gain, dtype, index, "k_gain", hd), eps, _at(row_pos, torch.int32, index, "row_pos", rows),
+            _at(freqs, torch.float64, index, "freqs", rot // 2), rot, ROPE_LAYOUTS[layout], rope_scale, qo, qos, ko, kos, pk,
+            pv, n_pages, _at(row_slot, torch.int32, index, "row_slot", rows))
     return q_out, k_out
 
 
@@ -651,33 +656,30 @@ def qk_norm_rope_backward(q: Optional[torch.Tensor], k: Optional[torch.Tensor], 
     """(dq, dk, dq_gain, dk_gain) of qk_norm_rope from its inputs and the gradients of its outputs
     (vla_qk_norm_rope_backward); the gains' gradients are fp32 [head_dim], None without the gain.  q and k may be None where
     they have no gain."""
-    lib = load_library()
-    dt, dev = _cache_dtype(dq_out), dq_out.device
-    rows, H, hd = dq_out.shape
-    K = dk_out.shape[1]
+    lib = _lib or load_library()
+    rows, H, hd, dt, index = _heads(dq_out, "dq_out")
+    dtype, dev, K = dq_out.dtype, dq_out.device, dk_out.shape[1]
     if dq is None:
-        dq = torch.empty((rows, H, hd), dtype=dq_out.dtype, device=dev)
+        dq = torch.empty((rows, H, hd), dtype=dtype, device=dev)
     if dk is None:
-        dk = torch.empty((rows, K, hd), dtype=dq_out.dtype, device=dev)
+        dk = torch.empty((rows, K, hd), dtype=dtype, device=dev)
     dq_gain = None if q_gain is None else torch.empty(hd, dtype=torch.float32, device=dev)
     dk_gain = None if k_gain is None else torch.empty(hd, dtype=torch.float32, device=dev)
     if workspace is None and (q_gain is not None or k_gain is not None):
         workspace = qk_norm_rope_workspace(dq_out)
-    rot = 0 if freqs is None else 2 * freqs.numel()
-    qp, qs = (None, 0) if q is None else _head_rows(q, dq_out, "q", H)
-    kp, ks = (None, 0) if k is None else _head_rows(k, dq_out, "k", K)
-    gq, gqs = _head_rows(dq_out, dq_out, "dq_out")
-    gk, gks = _head_rows(dk_out, dq_out, "dk_out", K)
-    oq, oqs = _head_rows(dq, dq_out, "dq", H)
-    ok, oks = _head_rows(dk, dq_out, "dk", K)
-    with _on(dev):
-        _check(lib.vla_qk_norm_rope_backward(
-            rows, H, K, hd, dt, qp, qs, kp, ks, gq, gqs, gk, gks, _at(q_gain, dq_out.dtype, dev, "q_gain", (hd,)),
-            _at(k_gain, dq_out.dtype, dev, "k_gain", (hd,)), eps, _at(row_pos, torch.int32, dev, "row_pos", (rows,)),
-            _at(freqs, torch.float64, dev, "freqs"), rot, ROPE_LAYOUTS[layout], rope_scale, oq, oqs, ok, oks,
-            None if dq_gain is None else dq_gain.data_ptr(), None if dk_gain is None else dk_gain.data_ptr(),
-            _at(workspace, torch.uint8, dev, "workspace"), 0 if workspace is None else workspace.numel(),
-            torch.cuda.current_stream(dev).cuda_stream))
+    qp, qs = (None, 0) if q is None else _head_rows(q, dtype, index, "q", rows, H, hd)
+    kp, ks = (None, 0) if k is None else _head_rows(k, dtype, index, "k", rows, K, hd)
+    gq, gqs = _head_rows(dq_out, dtype, index, "dq_out", rows, H, hd)
+    gk, gks = _head_rows(dk_out, dtype, index, "dk_out", rows, K, hd)
+    oq, oqs = _head_rows(dq, dtype, index, "dq", rows, H, hd)
+    ok, oks = _head_rows(dk, dtype, index, "dk", rows, K, hd)
+    rot = 0 if freqs is None else 2 * freqs.shape[0]
+    n_ws = 0 if workspace is None else workspace.shape[0]
+    _launch(index, lib.vla_qk_norm_rope_backward, rows, H, K, hd, dt, qp, qs, kp, ks, gq, gqs, gk, gks,
+            _at(q_gain, dtype, index, "q_gain", hd), _at(k_gain, dtype, index, "k_gain", hd), eps,
+            _at(row_pos, torch.int32, index, "row_pos", rows), _at(freqs, torch.float64, index, "freqs", rot // 2), rot,
+            ROPE_LAYOUTS[layout], rope_scale, oq, oqs, ok, oks, None if dq_gain is None else dq_gain.data_ptr(),
+            None if dk_gain is None else dk_gain.data_ptr(), _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
     return dq, dk, dq_gain, dk_gain
 
 
@@ -695,24 +697,19 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
                     lse: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention [n_env, n_heads, head_dim] of one token per environment over its lens[e] cached tokens
     (vla_paged_attention); lse fp32 [n_env, n_heads], if passed in, receives the log-sum-exp of the scores."""
-    lib = load_library()
-    dt, dev = _cache_dtype(q), q.device
-    n, H, hd = q.shape
+    lib = _lib or load_library()
+    n, H, hd, dt, index = _heads(q, "q")
+    dtype = q.dtype
     if out is None:
-        out = torch.empty((n, H, hd), dtype=q.dtype, device=dev)
-    qp, qs = _head_rows(q, q, "q")
-    op, os_ = _head_rows(out, q, "out", H)
-    pk, pv, n_pages, K = _pages(k_pages, v_pages, q)
-    if page_table.dtype != torch.int32 or page_table.device != dev or page_table.dim() != 2 or page_table.shape[0] != n \
-            or (page_table.shape[1] > 1 and page_table.stride(1) != 1):
-        raise ValueError("page_table must be int32 [n_env, max_pages] with contiguous rows")
-    max_pages = page_table.shape[1]
+        out = torch.empty((n, H, hd), dtype=dtype, device=q.device)
+    qp, qs = _head_rows(q, dtype, index, "q", n, H, hd)
+    op, os_ = _head_rows(out, dtype, index, "out", n, H, hd)
+    pk, pv, n_pages, K = _pool(k_pages, v_pages, dtype, index, hd)
+    table, ld, max_pages = _table(page_table, index, n)
     if workspace is None:
         workspace = paged_attention_workspace(q, k_pages, page_table)
-    with _on(dev):
-        _check(lib.vla_paged_attention(
-            n, H, K, hd, dt, qp, qs, pk, pv, n_pages, page_table.data_ptr() or None,
-            page_table.stride(0) if n > 1 else max_pages, max_pages, _at(lens, torch.int32, dev, "lens", (n,)), scale, op,
-            os_, _at(lse, torch.float32, dev, "lse", (n, H)), _at(workspace, torch.uint8, dev, "workspace"),
-            workspace.numel(), torch.cuda.current_stream(dev).cuda_stream))
+    n_ws = workspace.shape[0]
+    _launch(index, lib.vla_paged_attention, n, H, K, hd, dt, qp, qs, pk, pv, n_pages, table, ld, max_pages,
+            _at(lens, torch.int32, index, "lens", n), scale, op, os_, _at(lse, torch.float32, index, "lse", n, H),
+            _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
     return out
