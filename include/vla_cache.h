@@ -32,6 +32,7 @@
  * is rounded once, to nearest even.  Tensors start on 16 bytes; a row holds its
  * heads contiguously, and row strides (`ld_*`, in elements) are multiples of
  * 8 that hold a row, so q, k and v may be parts of one projection's output.
+ * At most 1024 heads and 1024 key heads.
  */
 #ifndef VLA_CACHE_H_
 #define VLA_CACHE_H_

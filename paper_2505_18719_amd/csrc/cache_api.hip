@@ -38,7 +38,7 @@ int check_rows(const char* name, const void* p, int64_t ld, int64_t width) {
 
 int check_heads(int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype) {
   if (n_heads < 1 || n_kv_heads < 1) return set_error(VLA_EINVAL, "need at least one head");
-  if (n_heads > 65535 || n_kv_heads > 65535) return set_error(VLA_EUNSUPPORTED, "at most 65535 heads");
+  if (n_heads > 1024 || n_kv_heads > 1024) return set_error(VLA_EUNSUPPORTED, "at most 1024 heads");
   if (head_dim != 64 && head_dim != 128 && head_dim != 256)
     return set_error(VLA_EUNSUPPORTED, "head_dim must be 64, 128 or 256");
   if (dtype != VLA_DTYPE_BF16 && dtype != VLA_DTYPE_F16) return set_error(VLA_EUNSUPPORTED, "unknown dtype");
