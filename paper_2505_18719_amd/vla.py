@@ -501,6 +501,7 @@ def logprob_backward(logits: torch.Tensor, tokens: torch.Tensor, action_begin: i
 CACHE_PAGE = 16
 CACHE_DTYPES = {torch.bfloat16: 0, torch.float16: 1}
 ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+PLAN_OUTPUTS = ("lens", "row_start", "row_pos", "row_env", "row_slot", "stats")
 ROPE_SCALINGS = ("none", "linear", "base", "bands", "ramp")
 
 
@@ -538,6 +539,14 @@ def _head_rows(t: torch.Tensor, dtype, index: int, name: str, rows: int, heads: 
     if sd != 1 or (sh != head_dim and heads > 1):
         raise ValueError(f"{name} must hold the heads of a row contiguously")
     return t.data_ptr() or None, (sr if rows > 1 else heads * head_dim)
+
+
+def _out_rows(t: Optional[torch.Tensor], like: torch.Tensor, index: int, name: str, rows: int, heads: int, head_dim: int):
+    """(tensor, address, row stride) of an output [rows, heads, head_dim], allocated here if there is none."""
+    if t is None:
+        t = torch.empty((rows, heads, head_dim), dtype=like.dtype, device=like.device)
+        return t, t.data_ptr() or None, heads * head_dim
+    return (t, *_head_rows(t, like.dtype, index, name, rows, heads, head_dim))
 
 
 def _heads(t: torch.Tensor, name: str):
@@ -590,14 +599,19 @@ def kv_plan(cached_lens: torch.Tensor, new_lens: torch.Tensor, page_table: torch
         raise ValueError("cached_lens [n_env] and free_pages [n_free] must be device tensors")
     n, n_free = cached_lens.shape[0], free_pages.shape[0]
     table, ld, max_pages = _table(page_table, index, n)
-    names, sizes = ("lens", "row_start", "row_pos", "row_env", "row_slot", "stats"), (n, n + 1, max_rows, max_rows, max_rows, 3)
+    sizes = (n, n + 1, max_rows, max_rows, max_rows, 3)
     if out is None:
         buf = torch.empty(sum(sizes), dtype=i32, device=cached_lens.device)
-        out = dict(zip(names, buf.split_with_sizes(sizes)))
+        out = dict(zip(PLAN_OUTPUTS, buf.split_with_sizes(sizes)))
+        lens = buf.data_ptr()  # never empty: stats
+        start = lens + 4 * n
+        pos = start + 4 * (n + 1)
+        places = (lens, start, pos, pos + 4 * max_rows, pos + 8 * max_rows, pos + 12 * max_rows)
+    else:
+        places = [_at(out[k], i32, index, k, s) for k, s in zip(PLAN_OUTPUTS, sizes)]
     _launch(index, lib.vla_kv_plan, n, _at(cached_lens, i32, index, "cached_lens", n),
             _at(new_lens, i32, index, "new_lens", n), table, ld, max_pages, _at(free_pages, i32, index, "free_pages", n_free),
-            n_free, _at(free_head, i32, index, "free_head", 1), n_pages, max_rows,
-            *[_at(out[k], i32, index, k, s) for k, s in zip(names, sizes)])
+            n_free, _at(free_head, i32, index, "free_head", 1), n_pages, max_rows, *places)
     return out
 
 
@@ -613,15 +627,13 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, row_pos: Optional[torch.Tenso
     lib = _lib or load_library()
     rows, H, hd, dt, index = _heads(q, "q")
     dtype, K = q.dtype, k.shape[1]
-    if q_out is None:
-        q_out = torch.empty((rows, H, hd), dtype=dtype, device=q.device)
-    if k_out is None and k_pages is None:
-        k_out = torch.empty((rows, K, hd), dtype=dtype, device=q.device)
+    q_out, qo, qos = _out_rows(q_out, q, index, "q_out", rows, H, hd)
+    ko, kos = None, 0
+    if k_out is not None or k_pages is None:
+        k_out, ko, kos = _out_rows(k_out, q, index, "k_out", rows, K, hd)
     qp, qs = _head_rows(q, dtype, index, "q", rows, H, hd)
     kp, ks = _head_rows(k, dtype, index, "k", rows, K, hd)
     vp, vs = (None, 0) if v is None else _head_rows(v, dtype, index, "v", rows, K, hd)
-    qo, qos = _head_rows(q_out, dtype, index, "q_out", rows, H, hd)
-    ko, kos = (None, 0) if k_out is None else _head_rows(k_out, dtype, index, "k_out", rows, K, hd)
     pk = pv = None
     n_pages = rot = 0
     if k_pages is not None:
@@ -659,10 +671,8 @@ def qk_norm_rope_backward(q: Optional[torch.Tensor], k: Optional[torch.Tensor], 
     lib = _lib or load_library()
     rows, H, hd, dt, index = _heads(dq_out, "dq_out")
     dtype, dev, K = dq_out.dtype, dq_out.device, dk_out.shape[1]
-    if dq is None:
-        dq = torch.empty((rows, H, hd), dtype=dtype, device=dev)
-    if dk is None:
-        dk = torch.empty((rows, K, hd), dtype=dtype, device=dev)
+    dq, oq, oqs = _out_rows(dq, dq_out, index, "dq", rows, H, hd)
+    dk, ok, oks = _out_rows(dk, dq_out, index, "dk", rows, K, hd)
     dq_gain = None if q_gain is None else torch.empty(hd, dtype=torch.float32, device=dev)
     dk_gain = None if k_gain is None else torch.empty(hd, dtype=torch.float32, device=dev)
     if workspace is None and (q_gain is not None or k_gain is not None):
@@ -671,8 +681,6 @@ def qk_norm_rope_backward(q: Optional[torch.Tensor], k: Optional[torch.Tensor], 
     kp, ks = (None, 0) if k is None else _head_rows(k, dtype, index, "k", rows, K, hd)
     gq, gqs = _head_rows(dq_out, dtype, index, "dq_out", rows, H, hd)
     gk, gks = _head_rows(dk_out, dtype, index, "dk_out", rows, K, hd)
-    oq, oqs = _head_rows(dq, dtype, index, "dq", rows, H, hd)
-    ok, oks = _head_rows(dk, dtype, index, "dk", rows, K, hd)
     rot = 0 if freqs is None else 2 * freqs.shape[0]
     n_ws = 0 if workspace is None else workspace.shape[0]
     _launch(index, lib.vla_qk_norm_rope_backward, rows, H, K, hd, dt, qp, qs, kp, ks, gq, gqs, gk, gks,
@@ -700,10 +708,8 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
     lib = _lib or load_library()
     n, H, hd, dt, index = _heads(q, "q")
     dtype = q.dtype
-    if out is None:
-        out = torch.empty((n, H, hd), dtype=dtype, device=q.device)
+    out, op, os_ = _out_rows(out, q, index, "out", n, H, hd)
     qp, qs = _head_rows(q, dtype, index, "q", n, H, hd)
-    op, os_ = _head_rows(out, dtype, index, "out", n, H, hd)
     pk, pv, n_pages, K = _pool(k_pages, v_pages, dtype, index, hd)
     table, ld, max_pages = _table(page_table, index, n)
     if workspace is None:
