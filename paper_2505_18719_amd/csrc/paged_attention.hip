@@ -387,11 +387,18 @@ __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a, int
 // while a step is taken, whatever piece it belongs to.  A piece inside a wave's run is written by the wave; what runs past
 // the run's ends is left in LDS, joined there with the neighbouring waves' parts, and what runs past the workgroup's ends
 // goes to the workspace: slot 2 w + 1 of workgroup w if the piece began there, else 2 w.  Who began a piece notes it down
-// for attn_join_kernel, which adds its partials in order.
+// for the kernel that then adds its partials in order.
 // Workgroups that the registers leave room for at once (64 x 4096 keys, 16 heads of 64: 254 us with 512, 174 with 1024).
 template <int HD, int QT>
 constexpr int kRunGroups = HD == 256 || (HD == 128 && QT == 2) ? 256 : HD == 64 && QT == 1 ? 1024 : 512;
 constexpr int kRunWaves = 4, kRunThreads = 64 * kRunWaves;  // the grid may be smaller than kRunGroups where the lengths cannot need it
+
+// Steps of a wave's run.
+template <int HD, int QT>
+__device__ __forceinline__ long long run_steps(long long units) {
+  constexpr unsigned kWavesAll = kRunGroups<HD, QT> * kRunWaves;
+  return max((long long)(((unsigned long long)units + kWavesAll - 1) / kWavesAll), 1ll);
+}
 
 struct SplitSpace {
   int4* begun;  // [groups] the piece that workgroup w began and did not end: environment, head block, last workgroup; or -1
@@ -455,8 +462,7 @@ __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, 
   }
   const int upto = wave_scan(mine);
   const long long units = (long long)__builtin_amdgcn_readlane(upto, kWave - 1) * blocks;
-  constexpr unsigned kWavesAll = kRunGroups<HD, QT> * kRunWaves;
-  const long long run = max((long long)(((unsigned long long)units + kWavesAll - 1) / kWavesAll), 1ll);  // steps of a wave
+  const long long run = run_steps<HD, QT>(units);
   const long long u0 = ((long long)me * kRunWaves + w) * run, first = (long long)(upto - mine) * blocks;
   const int n = __builtin_amdgcn_readfirstlane((int)max(0ll, min(run, units - u0)));
   int e = e0, len = len0;
@@ -582,21 +588,18 @@ __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, 
   }
 }
 
-// One workgroup per (workgroup of the run kernel, row of a head block): joins the piece that it began.
+// Adds the partials of a piece that workgroups w0 .. w0 + parts - 1 left, for row `row` of its head block and FW features
+// from f0 on.
 constexpr int kJoinThreads = 256;
-template <int HD, CacheType T, int QT>
-__global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a, SplitSpace sp, int rows) {
-  constexpr int PG = kJoinThreads * 4 / HD, NW = kJoinThreads / kWave;  // PG runs of partials are added side by side
+template <int HD, CacheType T, int QT, int FW>
+__device__ __forceinline__ void join_piece(const PagedAttnArgs& a, const SplitSpace& sp, int rows, int env, const HeadBlock& b, int row,
+                                           int w0, int parts, int f0) {
+  constexpr int PG = kJoinThreads * 4 / FW, NW = kJoinThreads / kWave;  // PG runs of partials are added side by side
   constexpr int PT = kRunGroups<HD, QT> / kJoinThreads;                 // partials per thread
   static_assert(kRunGroups<HD, QT> % kJoinThreads == 0, "partials are dealt out evenly");
-  __shared__ __align__(16) float so[PG][HD];
+  __shared__ __align__(16) float so[PG][FW];
   __shared__ float sc[kRunGroups<HD, QT>], sm[NW], sl[NW];
-  const int w0 = blockIdx.x, row = blockIdx.y, tid = threadIdx.x;
-  const int4 piece = sp.begun[w0];
-  if (piece.x < 0) return;
-  const HeadBlock b = head_block<QT>(a, piece.y);
-  if (row >= b.n) return;
-  const int parts = piece.z - w0 + 1;
+  const int tid = threadIdx.x;
   auto slot = [&](int i) { return 2 * (size_t)(w0 + i) + (i == 0 ? 1 : 0); };
   float mp[PT], lp[PT], m = -INFINITY, l = 0.f;
 #pragma unroll
@@ -625,11 +628,11 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
   l = wave_sum(l);
   if ((tid & 63) == 0) sl[tid >> 6] = l;
   __syncthreads();
-  const int f = 4 * (tid % (HD / 4)), pg = tid / (HD / 4);
+  const int f = 4 * (tid % (FW / 4)), pg = tid / (FW / 4);
   f32x4 v = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
   for (int i = pg; i < parts; i += PG) {
-    const f32x4 o = *reinterpret_cast<const f32x4*>(sp.o + (slot(i) * rows + row) * HD + f);
+    const f32x4 o = *reinterpret_cast<const f32x4*>(sp.o + (slot(i) * rows + row) * HD + f0 + f);
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], sc[i], v[e]);
   }
@@ -639,13 +642,46 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_kernel(PagedAttnArgs a
 #pragma unroll
   for (int i = 0; i < NW; ++i) l += sl[i];
   const float r = reciprocal(l);
-  if (tid < HD) {
+  if (tid < FW) {
     float t = 0.f;
 #pragma unroll
     for (int i = 0; i < PG; ++i) t += so[i][tid];
-    a.o[piece.x * a.ld_o + (size_t)(b.head0 + row) * HD + tid] = from_f32<T>(t * r);
+    a.o[env * a.ld_o + (size_t)(b.head0 + row) * HD + f0 + tid] = from_f32<T>(t * r);
   }
-  if (a.lse && tid == 0) a.lse[(size_t)piece.x * a.n_heads + b.head0 + row] = log_sum<T>(m, l);
+  if (a.lse && tid == 0 && f0 == 0) a.lse[(size_t)env * a.n_heads + b.head0 + row] = log_sum<T>(m, l);
+}
+
+// Where there are many pieces: one workgroup per workgroup of the run kernel and row of a head block, for the piece that it
+// began.
+template <int HD, CacheType T, int QT>
+__global__ __launch_bounds__(kJoinThreads) void attn_join_begun_kernel(PagedAttnArgs a, SplitSpace sp, int rows) {
+  const int w0 = blockIdx.x, row = blockIdx.y;
+  const int4 piece = sp.begun[w0];
+  if (piece.x < 0) return;
+  const HeadBlock b = head_block<QT>(a, piece.y);
+  if (row < b.n) join_piece<HD, T, QT, HD>(a, sp, rows, piece.x, b, row, w0, piece.z - w0 + 1, 0);
+}
+
+// Where there are few: one workgroup per piece, row of its head block and 64 features, which finds the piece's workgroups from
+// the lengths.
+template <int HD, CacheType T, int QT>
+__global__ __launch_bounds__(kJoinThreads) void attn_join_piece_kernel(PagedAttnArgs a, SplitSpace sp, int blocks, int rows) {
+  const int lane = threadIdx.x & 63, env = blockIdx.x / blocks, hb = blockIdx.x - env * blocks, row = blockIdx.y;
+  int all = 0, before = 0;
+  for (int e = lane; e < a.n_env; e += kWave) {
+    const int n = steps_of(a, a.lens[e]);
+    all += n;
+    before += e < env ? n : 0;
+  }
+  const int steps = steps_of(a, a.lens[env]);
+  const HeadBlock b = head_block<QT>(a, hb);
+  if (steps == 0 || row >= b.n) return;
+  all = __builtin_amdgcn_readlane(wave_scan(all), kWave - 1);
+  before = __builtin_amdgcn_readlane(wave_scan(before), kWave - 1);
+  const unsigned long long per = (unsigned long long)run_steps<HD, QT>((long long)all * blocks) * kRunWaves;
+  const unsigned long long u0 = (unsigned long long)before * blocks + (unsigned long long)hb * steps;
+  const int w0 = (int)(u0 / per), w1 = (int)((u0 + steps - 1) / per);
+  if (w0 < w1) join_piece<HD, T, QT, 64>(a, sp, rows, env, b, row, w0, w1 - w0 + 1, 64 * blockIdx.z);
 }
 
 // ------------------------------------------------------------------ host
@@ -672,7 +708,13 @@ hipError_t launch_run(const PagedAttnArgs& a, int blocks, int rows, hipStream_t 
   const int groups = (int)std::min((long long)kRunGroups<HD, QT>, (most + kRunWaves - 1) / kRunWaves);
   hipLaunchKernelGGL(kernel, dim3(groups), dim3(kRunThreads), Parts<HD>::bytes(2 * kRunWaves, rows), s, a, a.lens, a.page_table, sp,
                      blocks, rows);
-  hipLaunchKernelGGL((attn_join_kernel<HD, T, QT>), dim3(groups, rows), dim3(kJoinThreads), 0, s, a, sp, rows);
+  // Few pieces have many partials each (us of the join, by pieces / from the list: 2 pieces of 120 partials, heads of 256, 4.7 /
+  // 14.5; 8 of 64 4.4 / 5.7); of 512 pieces most workgroups would find nothing to do (64 x 4096 tokens in all 176 / 172).
+  const long long pieces = (long long)a.n_env * blocks;
+  if (pieces <= kRunGroups<HD, QT> / 4)
+    hipLaunchKernelGGL((attn_join_piece_kernel<HD, T, QT>), dim3((unsigned)pieces, rows, HD / 64), dim3(kJoinThreads), 0, s, a, sp, blocks, rows);
+  else
+    hipLaunchKernelGGL((attn_join_begun_kernel<HD, T, QT>), dim3(groups, rows), dim3(kJoinThreads), 0, s, a, sp, rows);
   return hipGetLastError();
 }
 
