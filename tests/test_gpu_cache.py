@@ -65,7 +65,7 @@ def make_tables(rng, cached, new, extra=2, spare=5):
     return table, pages[at:], need
 
 
-@pytest.mark.parametrize("n,ctx,most,seed", [(1, 0, 1, 0), (1, 37, 1, 1), (1, 15, 500, 2), (7, 40, 60, 3), (64, 400, 1, 4),
+@pytest.mark.parametrize("n,ctx,most,seed", [(255, 30, 9, 11), (256, 30, 9, 12), (257, 30, 9, 13), (1, 0, 1, 0), (1, 37, 1, 1), (1, 15, 500, 2), (7, 40, 60, 3), (64, 400, 1, 4),
                                              (300, 20, 40, 5), (1023, 50, 3, 6), (1024, 50, 3, 7), (1025, 50, 3, 8),
                                              (2500, 33, 9, 9), (3, 0, 70000, 10)])
 def test_plan(n, ctx, most, seed):
@@ -212,7 +212,7 @@ def test_norm_rope_outputs(cache, k_out, in_place, fused):
               seed=3)
 
 
-@pytest.mark.parametrize("rows", [2047, 2048, 5000])
+@pytest.mark.parametrize("rows", [511, 1025, 2047, 2048, 5000])
 @pytest.mark.parametrize("hd,K,dtype", [(64, 4, BF), (128, 8, FP), (256, 1, BF)])
 def test_norm_rope_many_rows(rows, hd, K, dtype):
     """On both sides of the split of a row's heads over waves; runs of slots at an odd offset, and scattered ones."""
@@ -293,6 +293,12 @@ def test_norm_rope_backward(rows, H, K, hd, rot, layout, dtype):
     back_case(rows, H, K, hd, rot, layout, dtype, seed=rows)
 
 
+@pytest.mark.parametrize("hd,K,layout", [(128, 8, "half"), (256, 2, "interleaved"), (64, 16, "half")])
+def test_norm_rope_backward_of_many_rows(hd, K, layout):
+    """Several tiles of rows to a workgroup, and more bytes than the caches are asked to keep."""
+    back_case(9001, 3 * K, K, hd, hd, layout, BF, seed=5)
+
+
 @pytest.mark.parametrize("norm", [(True, False), (False, True), (False, False)])
 @pytest.mark.parametrize("fused,in_place", [(True, True), (False, False)])
 def test_norm_rope_backward_gains_apart_and_in_place(norm, fused, in_place):
@@ -360,8 +366,8 @@ def check_attention(got, lse, q, kp, vp, table, lens, scale, envs=None):
     return bad.max()
 
 
-def attn_case(lens, H, K, hd, dtype, seed=0, qscale=2.0, strided=False):
-    kp, vp, table, lens = make_cache(lens, K, hd, dtype, seed)
+def attn_case(lens, H, K, hd, dtype, seed=0, qscale=2.0, strided=False, extra_cols=1):
+    kp, vp, table, lens = make_cache(lens, K, hd, dtype, seed, extra_cols=extra_cols)
     n, scale = len(lens), hd ** -0.5
     if strided:
         q = rand((n, (H + 2) * hd), dtype, seed + 2, qscale)[:, hd:(H + 1) * hd].unflatten(1, (H, hd))
@@ -389,6 +395,22 @@ EDGES = [0, 1, 2, 15, 16, 17, 31, 32, 33, 47, 63, 64, 65, 100, 127, 128, 129, 25
 @pytest.mark.parametrize("H,K", [(1, 1), (7, 7), (8, 2), (28, 4), (16, 1), (17, 1), (40, 1), (64, 1)])
 def test_attention_lengths_and_groups(hd, dtype, H, K):
     attn_case(EDGES, H, K, hd, dtype, seed=H + K)
+
+
+@pytest.mark.parametrize("hd", [64, 128, 256])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("H,K", [(1, 1), (7, 7), (8, 2), (28, 4), (17, 1), (40, 1)])
+def test_attention_with_room_in_the_table(hd, dtype, H, K):
+    """The same lengths in a table with room for more: the keys are split, and nothing of the unused columns is read."""
+    attn_case(EDGES, H, K, hd, dtype, seed=H + K, extra_cols=40)
+
+
+@pytest.mark.parametrize("extra_cols", [1, 40])
+@pytest.mark.parametrize("lens,H,K,hd,dtype", [(EDGES * 7, 16, 8, 128, BF), (EDGES * 3, 32, 32, 64, FP), (EDGES * 13, 4, 4, 256, FP),
+                                               ([700, 3, 0, 90] * 20, 8, 8, 128, FP), ([1] * 1100, 2, 1, 64, BF)])
+def test_attention_of_many_environments(lens, H, K, hd, dtype, extra_cols):
+    """From about 1000 key heads in all on, a wave takes one by itself; split, pieces begin and end anywhere in a wave's run."""
+    attn_case(lens, H, K, hd, dtype, seed=len(lens), extra_cols=extra_cols)
 
 
 @pytest.mark.parametrize("n", [1, 2, 3])
@@ -617,6 +639,22 @@ def test_a_captured_step_grows_the_cache():
         assert plan["lens"].tolist() == [len(h) for h in hist]
         assert np.all(np.abs(f64(att) - ref) <= tol), i
         torch.randn(1000, device="cuda").sum().item()
+
+
+def test_a_first_call_may_be_captured():
+    """A shape that nothing has run before, in a graph at once (its workgroups take more LDS than a kernel has by default)."""
+    kp, vp, table, lens = make_cache([700, 31], 1, 128, FP, 9)
+    q, t, n = rand((2, 24, 128), FP, 10), i32(table), i32(lens)
+    ws, out = vla.paged_attention_workspace(q, kp, t), torch.empty(2, 24, 128, dtype=FP, device="cuda")
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        vla.paged_attention(q, kp, vp, t, n, 0.1, out=out, workspace=ws)
+    for i in range(3):
+        out.zero_()
+        n.copy_(i32([lens[0] - 300 * i, lens[1] - i]))
+        g.replay()
+        check_attention(out, None, q, kp, vp, table, [lens[0] - 300 * i, lens[1] - i], 0.1)
 
 
 def test_calls_on_another_stream():
