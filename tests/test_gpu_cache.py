@@ -441,6 +441,25 @@ def test_attention_of_one_strong_key_among_weak_ones(n, dtype):
     check_attention(got, None, q, kp, vp, table, lens, 1.0)
 
 
+@pytest.mark.parametrize("dtype", [BF, FP])
+def test_attention_tail_of_tiny_weights(dtype):
+    """200000 keys of weights 2^-29.2 of the strongest key's, whose value is zero: the output is theirs alone."""
+    hd, n = 64, 200001
+    kp, vp, table, lens = make_cache([n], 1, hd, dtype, 3)
+    q = torch.zeros(1, 1, hd, dtype=dtype, device="cuda")
+    q[..., 0] = 20.3125
+    kp[..., 0] = 0.0
+    kp[table[0, 0], 0, 0, 0] = 1.0
+    vp[:] = torch.where(torch.isfinite(vp), 1.0, vp)
+    vp[table[0, 0], 0, :, 0] = 0.0
+    got = f64(vla.paged_attention(q, kp, vp, i32(table), i32(lens), 1.0))
+    w = (n - 1) * math.exp(-float(q[0, 0, 0]))  # bf16 holds 20.25
+    ref = np.full(got.shape, w / (1 + w))
+    # half-precision weights are whole multiples of 2^-39 of the largest (bf16 pairs: 16 bits of each)
+    weights = (n - 1) * 2.0 ** -40 if dtype is FP else 2.0 ** -16 * ref
+    assert np.all(np.abs(got - ref) <= half_step(ref, dtype) * (1 + 2 ** -6) + weights + 2 * (hd + 32) * U32 * 20.4 * ref)
+
+
 def test_attention_counts_every_key_once():
     """Equal scores: the mean of the values, whose integers fp32 adds exactly."""
     for n in (1, 5, 16, 1000, 4097):
