@@ -718,19 +718,21 @@ hipError_t launch_run(const PagedAttnArgs& a, int blocks, int rows, hipStream_t 
   return hipGetLastError();
 }
 
-// Up to 512 tokens the two launches of the split cost more than they save, whatever the number of items (GPU us, whole /
-// split: 278 tokens, 32 key heads 7.6 / 10.3; 512 tokens, 8 key heads 9.4 / 9.6; 64 x 300, 8 key heads 16 / 25); beyond, the
-// split is as fast where items abound and faster where they are few or uneven (1024 tokens, 8 key heads 16.9 / 9.8; 64 of
-// up to 2048 56 / 54).
-bool split_keys(int max_pages) { return max_pages > 32; }
+// Whether the keys are split, of `pieces` environments and head blocks.  Short keys are taken whole: the split's second launch
+// and its way through the workspace cost more than they save (GPU us, whole / split: 1 x 278 tokens, 32 pieces, 6.2 / 10; 1 x
+// 512, 8 pieces, 7.5 / 9.1), up to 1024 tokens where there are pieces enough to fill half the GPU (32 x 700 tokens, 256 pieces,
+// 17.9 / 25.6; 16 of up to 1024, 128 pieces, 12.7 / 15.1; but 8 x 1024, 64 pieces, 18 / 14.3).  Beyond, the split is as fast where
+// pieces abound and faster where they are few or uneven (1 x 1024 16.9 / 9.3; 64 of up to 2048 53.8 / 52.7).
+bool split_keys(long long pieces, int max_pages) { return max_pages > (pieces >= 128 ? 64 : 32); }
 
 template <int HD, CacheType T, int QT, bool STREAM>
 hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
   const int group = a.n_heads / a.n_kv_heads, blocks = head_blocks<QT>(group) * a.n_kv_heads, rows = query_rows(group, QT);
-  if (split_keys(a.max_pages)) return launch_run<HD, T, QT, STREAM>(a, blocks, rows, s);
-  // One wave per item where those fill the GPU, else four (us, one / four: 512 x 30 tokens, 8 key heads 16 / 28; 512 x 128
-  // 47 / 53; 64 x 300, 32 key heads 52.9 / 54; 512 items of 300 tokens 16.9 / 16.2, 256 of 64 5.2 / 4.7)
-  if ((long long)blocks * a.n_env >= 1024) return launch_whole<HD, T, QT, STREAM, 1>(a, blocks, rows, s);
+  const long long pieces = (long long)a.n_env * blocks;
+  if (split_keys(pieces, a.max_pages)) return launch_run<HD, T, QT, STREAM>(a, blocks, rows, s);
+  // One wave per piece where those fill the GPU, else four (us, one / four: 512 x 30 tokens, 8 key heads 16 / 28; 512 x 128
+  // 47 / 53; 64 x 300, 32 key heads 52.9 / 54; 512 pieces of 300 tokens 16.9 / 16.2, 256 of 64 5.2 / 4.7)
+  if (pieces >= 1024) return launch_whole<HD, T, QT, STREAM, 1>(a, blocks, rows, s);
   return launch_whole<HD, T, QT, STREAM, 4>(a, blocks, rows, s);
 }
 
@@ -764,9 +766,10 @@ hipError_t launch_type(const PagedAttnArgs& a, hipStream_t s) {
 
 }  // namespace
 
-size_t paged_attn_bytes(int, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
-  if (!split_keys(max_pages)) return 256;
+size_t paged_attn_bytes(int n_env, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
   const int group = n_heads / n_kv_heads, tiles = query_tiles(group, head_dim), rows = query_rows(group, tiles);
+  const int blocks = (tiles == 1 ? head_blocks<1>(group) : head_blocks<2>(group)) * n_kv_heads;
+  if (!split_keys((long long)n_env * blocks, max_pages)) return 256;
   if (head_dim == 64) return tiles == 1 ? split_bytes<64, 1>(rows) : split_bytes<64, 2>(rows);
   if (head_dim == 128) return tiles == 1 ? split_bytes<128, 1>(rows) : split_bytes<128, 2>(rows);
   return split_bytes<256, 1>(rows);

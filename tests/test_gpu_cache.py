@@ -402,10 +402,10 @@ def test_attention_lengths_and_groups(hd, dtype, H, K):
 @pytest.mark.parametrize("H,K", [(1, 1), (7, 7), (8, 2), (28, 4), (17, 1), (40, 1)])
 def test_attention_with_room_in_the_table(hd, dtype, H, K):
     """The same lengths in a table with room for more: the keys are split, and nothing of the unused columns is read."""
-    attn_case(EDGES, H, K, hd, dtype, seed=H + K, extra_cols=40)
+    attn_case(EDGES, H, K, hd, dtype, seed=H + K, extra_cols=80)
 
 
-@pytest.mark.parametrize("extra_cols", [1, 40])
+@pytest.mark.parametrize("extra_cols", [1, 80])
 @pytest.mark.parametrize("lens,H,K,hd,dtype", [(EDGES * 7, 16, 8, 128, BF), (EDGES * 3, 32, 32, 64, FP), (EDGES * 13, 4, 4, 256, FP),
                                                ([700, 3, 0, 90] * 20, 8, 8, 128, FP), ([1] * 1100, 2, 1, 64, BF)])
 def test_attention_of_many_environments(lens, H, K, hd, dtype, extra_cols):
