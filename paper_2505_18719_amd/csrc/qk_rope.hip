@@ -4,7 +4,7 @@
 // Bound: HBM, every feature read once and written once (the gradient: two read, one written).  A head vector is held by
 // head_dim / 16 lanes, 16 features each, placed so that both features of every pair are in one lane: the norm is a sum over
 // 4, 8 or 16 lanes by DPP, the rotation needs no exchange.  Measured at 32 + 8 heads of 128: 18432 rows appended in 85 us, 453
-// MB, 5.3 TB/s (a copy of 1 GiB: 5.2); the gradient of 18880 rows 117 us, 580 MB, 5.0 TB/s; one row 3.1 us.
+// MB, 5.3 TB/s (a copy of 1 GiB: 5.2); the gradient of 18880 rows 112 us, 580 MB, 5.2 TB/s; one row 3.1 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -215,6 +215,8 @@ __device__ __forceinline__ void append_v(const QkRopeArgs& a, long long row0, in
     const int r = lane / 8 + i * 8;
     if (r >= r0 && r < end && (lives >> r & 1)) *reinterpret_cast<uint4*>(&tile.x[r][8 * (lane % 8)]) = load16<false>(src + i * 8 * a.v.ld);
   }
+  // written by other lanes and as another type: the reads below stay behind the writes (no instruction, LDS is in order)
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
   __builtin_amdgcn_wave_barrier();
   // feature `first` of slot s: head first / HD, its feature first % HD
   auto at = [&](int s) { return a.pages.v + ((long long)(s / kPage) * a.n_kv_heads * HD + first) * kPage + s % kPage; };
@@ -299,8 +301,7 @@ struct Angles {
 // 31.5 / 121.1, 33.9 / 129.2, 38.3).
 constexpr int kBwdGroups = 512;
 
-// A workgroup goes over tiles of rows, all of them side by side in memory; the gains' gradients of its lanes' features stay in registers, are joined over the
-// workgroup and left in part[group][q or k][feature].
+// The gradient of a tile's queries or of its keys.
 template <int HD, CacheType T, int LAYOUT, bool STREAM>
 struct Backward {
   static constexpr int LPH = HD / 16, VPP = kRopeThreads / LPH;  // lanes per head vector, vectors per pass
@@ -309,35 +310,41 @@ struct Backward {
     uint4 d[2], x[2];
     int row, head;
   };
-  // The vectors of one tile's queries (or keys); the next pass's are on their way while one is taken.
-  static __device__ __forceinline__ void tile(const QkRopeBwdArgs& a, const Angles<HD>& angles, const Chunks<HD, LAYOUT>& ch, long long row0,
-                                              int rows, int heads, unsigned magic, const HeadRows& in, const HeadRows& dout,
-                                              const HeadRows& out, const bf16_t* gain, float (&dg)[16]) {
+  const Chunks<HD, LAYOUT>& ch;
+  HeadRows in, dout, out;
+  const bf16_t* gain;
+  int heads;
+  unsigned magic;
+  float eps;
+
+  __device__ __forceinline__ void load(Vector& u, long long row0, int v) const {
+    u.row = div_by(v, magic);
+    u.head = v - u.row * heads;
+    const bf16_t* p = dout.p + (row0 + u.row) * dout.ld + u.head * HD;
+    u.d[0] = load16<STREAM>(p + ch.lo);
+    u.d[1] = load16<STREAM>(p + ch.hi);
+    if (gain) {
+      p = in.p + (row0 + u.row) * in.ld + u.head * HD;
+      u.x[0] = load16<STREAM>(p + ch.lo);
+      u.x[1] = load16<STREAM>(p + ch.hi);
+    }
+  }
+  // The first pass's vector of a tile, on its way before the tile's angles are known.
+  __device__ __forceinline__ void start(Vector& u, long long row0, int rows) const {
+    const int v = threadIdx.x / LPH;
+    if (v < rows * heads) load(u, row0, v);
+  }
+  // All passes from `cur` on; the next pass's vector is on its way while one is taken.
+  __device__ __forceinline__ void tile(Vector cur, const Angles<HD>& angles, long long row0, int rows, float (&dg)[16]) const {
     const int vectors = rows * heads;
     uint4 w[2];
     if (gain) {
       w[0] = *reinterpret_cast<const uint4*>(gain + ch.lo);
       w[1] = *reinterpret_cast<const uint4*>(gain + ch.hi);
     }
-    auto load = [&](Vector& u, int v) {
-      u.row = div_by(v, magic);
-      u.head = v - u.row * heads;
-      const bf16_t* p = dout.p + (row0 + u.row) * dout.ld + u.head * HD;
-      u.d[0] = load16<STREAM>(p + ch.lo);
-      u.d[1] = load16<STREAM>(p + ch.hi);
-      if (gain) {
-        p = in.p + (row0 + u.row) * in.ld + u.head * HD;
-        u.x[0] = load16<STREAM>(p + ch.lo);
-        u.x[1] = load16<STREAM>(p + ch.hi);
-      }
-    };
-    int v = threadIdx.x / LPH;
-    if (v >= vectors) return;
-    Vector cur, next;
-    load(cur, v);
-    for (; v < vectors; v += VPP) {
-      next = cur;
-      if (v + VPP < vectors) load(next, v + VPP);
+    for (int v = threadIdx.x / LPH; v < vectors; v += VPP) {
+      Vector next = cur;
+      if (v + VPP < vectors) load(next, row0, v + VPP);
       float y[16];
       unpack<T>(cur.d[0], y);
       unpack<T>(cur.d[1], y + 8);
@@ -350,7 +357,7 @@ struct Backward {
         unpack<T>(cur.x[1], h + 8);
 #pragma unroll
         for (int e = 0; e < 16; ++e) ss = fmaf(h[e], h[e], ss);
-        const float r = rsqrtf(group_sum<LPH>(ss) * (1.f / HD) + a.eps);
+        const float r = rsqrtf(group_sum<LPH>(ss) * (1.f / HD) + eps);
         float dot = 0.f;
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
@@ -371,6 +378,20 @@ struct Backward {
   }
 };
 
+// Sum over the lanes that share lane % N (N = 4, 8, 16).
+template <int N>
+__device__ __forceinline__ float across_sum(float v) {
+  if constexpr (N <= 8) v += dpp_mov<0x128>(v, v);  // 8 lanes on in the 16
+  if constexpr (N <= 4) v += dpp_mov<0x124>(v, v);  // 4 lanes on
+  auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+  r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// A workgroup goes over tiles of rows, all of them side by side in memory; the gains' gradients of its lanes' features stay
+// in registers, are joined over the workgroup and left in part[group][q or k][feature].  A tile's first queries are
+// requested before its angles are made (18880 and 300 rows of 32 + 8 heads: 117.5 -> 115.6, 12.3 -> 10.7 us).
 template <int HD, CacheType T, int LAYOUT, bool STREAM>
 __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(QkRopeBwdArgs a, int tile, unsigned magic_q, unsigned magic_k) {
   using B = Backward<HD, T, LAYOUT, STREAM>;
@@ -378,27 +399,30 @@ __global__ __launch_bounds__(kRopeThreads) void qk_rope_bwd_kernel(QkRopeBwdArgs
   __shared__ float red[kRopeWaves][2][HD];
   const int lane = threadIdx.x & 63, w = threadIdx.x >> 6, j = threadIdx.x % B::LPH;
   const Chunks<HD, LAYOUT> ch(j, a.rot_dim);
+  const B q = {ch, a.q, a.dq_out, a.dq, a.q_gain, a.n_heads, magic_q, a.eps};
+  const B k = {ch, a.k, a.dk_out, a.dk, a.k_gain, a.n_kv_heads, magic_k, a.eps};
   float dg[2][16];
 #pragma unroll
   for (int e = 0; e < 16; ++e) dg[0][e] = dg[1][e] = 0.f;
   for (long long row0 = (long long)blockIdx.x * tile; row0 < a.rows; row0 += (long long)gridDim.x * tile) {
     const int rows = (int)min((long long)tile, a.rows - row0);
+    typename B::Vector vq, vk;
+    q.start(vq, row0, rows);
     if (a.rot_dim > 0) {
       __syncthreads();  // the last tile's angles have been read
-      angles.fill(a.freqs, a.row_pos, a.rot_dim / 2, a.rope_scale, (int)row0, rows);
+      angles.fill(a.freqs, a.row_pos, a.rot_dim / 2, a.rope_scale, row0, rows);
       __syncthreads();
     }
-    B::tile(a, angles, ch, row0, rows, a.n_heads, magic_q, a.q, a.dq_out, a.dq, a.q_gain, dg[0]);
-    B::tile(a, angles, ch, row0, rows, a.n_kv_heads, magic_k, a.k, a.dk_out, a.dk, a.k_gain, dg[1]);
+    q.tile(vq, angles, row0, rows, dg[0]);
+    k.start(vk, row0, rows);
+    k.tile(vk, angles, row0, rows, dg[1]);
   }
   if (!a.q_gain && !a.k_gain) return;
 #pragma unroll
   for (int t = 0; t < 2; ++t)
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
-      float v = dg[t][e];
-#pragma unroll
-      for (int o = B::LPH; o < kWave; o <<= 1) v += __shfl_xor(v, o, kWave);
+      const float v = across_sum<B::LPH>(dg[t][e]);
       if (lane < B::LPH) red[w][t][(e < 8 ? ch.lo : ch.hi) + e % 8] = v;
     }
   __syncthreads();

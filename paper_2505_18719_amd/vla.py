@@ -640,6 +640,8 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, row_pos: Optional[torch.Tenso
         pk, pv, n_pages, kv = _pool(k_pages, v_pages, dtype, index, hd)
         if kv != K:
             raise ValueError("the pages must have the heads of k")
+    elif v_pages is not None:
+        raise ValueError("v_pages without k_pages")
     if freqs is not None:
         rot = 2 * freqs.shape[0]
     if rows == 0:

@@ -734,6 +734,7 @@ def test_binding_refusals():
                 lambda: vla.paged_attention(q, kp, vp, i32(table).long(), i32(lens), 0.1),
                 lambda: vla.qk_norm_rope(q, q[:, :, ::2], i32([0]), vla.rope_freqs(64)[0]),
                 lambda: vla.qk_norm_rope(q, q, i32([0, 1]), vla.rope_freqs(64)[0]),
+                lambda: vla.qk_norm_rope(q, q, i32([0]), vla.rope_freqs(64)[0], v_pages=vp),
                 lambda: vla.qk_norm_rope_backward(q, q, q, q, i32([0]), vla.rope_freqs(64)[0].float())):
         with pytest.raises(ValueError):
             bad()
