@@ -334,7 +334,8 @@ template <int HD, CacheType T>
 __device__ __forceinline__ void no_keys(const PagedAttnArgs& a, int env, int head0, int n, int len) {
   const float v = len == 0 ? 0.f : __builtin_nanf("");
   for (int i = threadIdx.x; i < n * HD; i += blockDim.x) a.o[env * a.ld_o + (size_t)head0 * HD + i] = from_f32<T>(v);
-  if (a.lse && (int)threadIdx.x < n) a.lse[(size_t)env * a.n_heads + head0 + threadIdx.x] = len == 0 ? -INFINITY : v;
+  if (a.lse)  // n may be all heads of an environment, more than there are threads
+    for (int i = threadIdx.x; i < n; i += blockDim.x) a.lse[(size_t)env * a.n_heads + head0 + i] = len == 0 ? -INFINITY : v;
 }
 
 // One workgroup of W waves per (head block, environment); wave w takes steps w, w + W, ...
