@@ -277,14 +277,17 @@ struct Parts {
   }
 };
 
+// 1 / l, or 0 where no score is above -inf; then the output is zeros, also where a value times its weight of 0 is NaN.
+__device__ __forceinline__ float reciprocal(float l) { return l == 0.f ? 0.f : 1.f / l; }
+template <CacheType T>
+__device__ __forceinline__ bf16_t output(float o, float r) { return from_f32<T>(r == 0.f ? 0.f : o * r); }
 template <CacheType T>
 __device__ __forceinline__ void store4(bf16_t* p, const f32x4& v, float r) {
   bf16_t h[4];
 #pragma unroll
-  for (int e = 0; e < 4; ++e) h[e] = from_f32<T>(v[e] * r);
+  for (int e = 0; e < 4; ++e) h[e] = output<T>(v[e], r);
   *reinterpret_cast<uint2*>(p) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
 }
-__device__ __forceinline__ float reciprocal(float l) { return l == 0.f ? 0.f : 1.f / l; }  // no score above -inf: zeros
 
 // Adds parts first, first + step, ... (N of them) by the whole workgroup.
 template <int HD, CacheType T, int N>
@@ -647,7 +650,7 @@ __device__ __forceinline__ void join_piece(const PagedAttnArgs& a, const SplitSp
     float t = 0.f;
 #pragma unroll
     for (int i = 0; i < PG; ++i) t += so[i][tid];
-    a.o[env * a.ld_o + (size_t)(b.head0 + row) * HD + f0 + tid] = from_f32<T>(t * r);
+    a.o[env * a.ld_o + (size_t)(b.head0 + row) * HD + f0 + tid] = output<T>(t, r);
   }
   if (a.lse && tid == 0 && f0 == 0) a.lse[(size_t)env * a.n_heads + b.head0 + row] = log_sum<T>(m, l);
 }

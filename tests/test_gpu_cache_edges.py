@@ -35,3 +35,30 @@ def test_lse_of_every_head_without_a_pool():
     got = vla.paged_attention(q, kp, vp, torch.zeros(3, 99, dtype=torch.int32, device="cuda"), i32([1, 0, 1500]), 0.1, lse=lse)
     assert (got[1] == 0).all() and (lse[1] == -math.inf).all()
     assert got[::2].isnan().all() and lse[::2].isnan().all()
+
+
+# ------------------------------------------------------------------ infinite and NaN values
+# (environments' lengths, heads, key heads, head_dim, columns of the table past the lengths): taken whole by four waves and by
+# one, split with a piece in many workgroups, split with many pieces in a wave's run
+PATHS = [([90, 33, 1, 500], 8, 2, 128, 1), ([40, 3, 100] * 100, 4, 4, 64, 1), ([3000, 0, 700], 8, 2, 128, 1),
+         ([40, 3, 100, 17] * 300, 4, 2, 64, 80), ([900, 70], 6, 1, 256, 1), ([50, 400], 40, 1, 64, 1), ([60, 5000], 40, 1, 128, 1)]
+
+
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("lens,H,K,hd,extra_cols", PATHS)
+def test_heads_without_a_score_are_zeros_whatever_the_values(lens, H, K, hd, extra_cols, dtype):
+    """Every score of the odd key heads is -inf: zeros, with infinities and NaN among the values; the even ones are as ever."""
+    kp, vp, table, lens = make_cache(lens, K, hd, dtype, 3, extra_cols=extra_cols)
+    q = rand((len(lens), H, hd), dtype, 4)
+    q[..., 0] = 1.0
+    odd = np.arange(H) * K // H % 2 == 1 if K > 1 else np.full(H, True)
+    keys = slice(1, None, 2) if K > 1 else slice(None)
+    kp[:, keys, :, 0] = -math.inf
+    vp[:, keys, 0::3] = math.inf
+    vp[:, keys, 1::3] = math.nan
+    lse = torch.empty(len(lens), H, device="cuda")
+    got = vla.paged_attention(q, kp, vp, i32(table), i32(lens), hd ** -0.5, lse=lse)
+    assert (got[:, odd] == 0).all() and (lse[:, odd] == -math.inf).all()
+    if K > 1:
+        even = np.arange(K) % 2 == 0
+        check_attention(got[:, ~odd], lse[:, ~odd], q[:, ~odd], kp[:, even], vp[:, even], table, lens, hd ** -0.5)
