@@ -161,9 +161,11 @@ int vla_qk_norm_rope_backward(int32_t rows, int32_t n_heads, int32_t n_kv_heads,
  * n_kv_heads / n_heads (rounded down),
  *     out[e, h] = sum_j p_j v_j,  p = softmax_j(scale q[e, h] . k_j).
  * An environment of length 0 gets zeros, as does a head all of whose scores
- * are -inf; a NaN among them gives NaN.  What the last page holds past the
- * length does not matter, nor do the table's entries past the last page.  A
- * length below 0 or above 16 * max_pages, or a page outside [0, n_pages)
+ * are -inf, whatever its values; a NaN or +inf among them gives NaN.  An
+ * infinite value makes its feature's sum infinite however small its weight,
+ * and NaN beside one of the other sign or at a score of -inf.  What the last
+ * page holds past the length does not matter, nor do the table's entries past
+ * the last page.  A length below 0 or above 16 * max_pages, or a page outside [0, n_pages)
  * among those of the length, gives an environment of NaN (nothing outside the
  * pool is read).
  *   q, out       [n_env, n_heads, head_dim] (row strides ld_q, ld_o); head_dim

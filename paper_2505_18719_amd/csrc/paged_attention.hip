@@ -35,6 +35,16 @@ __device__ __forceinline__ bf16_t from_f32(float f) {
   else return __builtin_bit_cast(bf16_t, (_Float16)f);
 }
 
+// Those of the two numbers in x that are infinite or NaN, 0 in the place of the others.
+template <CacheType T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t x) {
+  constexpr uint32_t kExp = T == kBf16 ? 0x7f80 : 0x7c00;
+  return ((x & kExp) == kExp ? x & 0xffffu : 0u) | ((x & kExp << 16) == kExp << 16 ? x & 0xffff0000u : 0u);
+}
+// What the sums under a base-2 maximum m are worth under a larger one: at least 2^-149, so that an infinity among them stays one
+// (finite sums lose nothing: 2^-149 of them does not show).
+__device__ __forceinline__ float worth(float m, float larger) { return fmaxf(__builtin_amdgcn_exp2f(m - larger), 0x1p-149f); }
+
 // hi + lo = p[0 .. 8) to the precision of two numbers of the type
 template <CacheType T>
 __device__ __forceinline__ void split_weights(const float* p, uint4& hi, uint4& lo) {
@@ -175,7 +185,7 @@ struct Wave {
     for (int i = 0; i < VC; ++i) v[i] = load_page<STREAM>(p + 16 * i * kPage);
   }
 
-  // p = base-2 scores of the step's keys; k and q are free afterwards
+  // p = base-2 scores of the step's keys; k is free afterwards
   __device__ __forceinline__ void scores(float (&p)[QT][8]) {
 #pragma unroll
     for (int t = 0; t < QT; ++t)
@@ -188,9 +198,12 @@ struct Wave {
         for (int r = 0; r < 4; ++r) p[t][4 * u + r] = c[r] * scale;
       }
   }
-  // Takes the step's keys, of which `left` (< 32: the last step) count, into the running sums; v is free afterwards.
+  // Takes the step's keys, of which `left` (< 32: the last step) count, into the running sums; v is free afterwards.  APART:
+  // values that are infinite or NaN are taken by weights of 1 (0 at scores of -inf), apart from the finite ones: an infinity
+  // times a weight's lo part of 0 or below is no part of the sum, nor is one times a weight that rounds to 0.
+  template <bool APART>
   __device__ __forceinline__ void weigh(float (&p)[QT][8], int left) {
-    uint4 hi[QT], lo[QT];
+    uint4 hi[QT], lo[QT], one[QT];
 #pragma unroll
     for (int t = 0; t < QT; ++t) {
       if (left < kStep) {
@@ -203,11 +216,18 @@ struct Wave {
       for (int j = 1; j < 8; ++j) mx = fmaxf(mx, p[t][j]);
       mx = fmaxf(run.m[t], column_max(mx));
       if (__any(mx > run.m[t])) {  // seldom after the first steps
-        const float c = run.m[t] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(run.m[t] - mx);  // nothing to scale yet: 1
+        const float c = run.m[t] == -INFINITY ? 1.f : worth(run.m[t], mx);  // nothing to scale yet: 1
         run.l[t] *= c;
 #pragma unroll
         for (int i = 0; i < VC; ++i) run.o[t][i] *= c;
         run.m[t] = mx;
+      }
+      if constexpr (APART) {
+        constexpr uint32_t k1 = T == kBf16 ? 0x3f80 : 0x3c00;
+        uint32_t d[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) d[j] = (p[t][2 * j] > -INFINITY ? k1 : 0) | (p[t][2 * j + 1] > -INFINITY ? k1 << 16 : 0);
+        one[t] = make_uint4(d[0], d[1], d[2], d[3]);
       }
       const float base = run.m[t] == -INFINITY ? 0.f : run.m[t] - kWeightExp<T>;
       float sum = 0.f;
@@ -228,17 +248,49 @@ struct Wave {
       for (int i = 0; i < VC; ++i) v[i] = make_uint4(v[i].x & keep[0], v[i].y & keep[1], v[i].z & keep[2], v[i].w & keep[3]);
     }
 #pragma unroll
-    for (int i = 0; i < VC; ++i)
+    for (int i = 0; i < VC; ++i) {
+      uint4 rest;
+      if constexpr (APART) {
+        rest = make_uint4(not_finite<T>(v[i].x), not_finite<T>(v[i].y), not_finite<T>(v[i].z), not_finite<T>(v[i].w));
+        v[i] = make_uint4(v[i].x ^ rest.x, v[i].y ^ rest.y, v[i].z ^ rest.z, v[i].w ^ rest.w);
+      }
 #pragma unroll
       for (int t = 0; t < QT; ++t) {
         run.o[t][i] = mfma<T>(v[i], hi[t], run.o[t][i]);
         run.o[t][i] = mfma<T>(v[i], lo[t], run.o[t][i]);
+        if constexpr (APART) run.o[t][i] = mfma<T>(rest, one[t], run.o[t][i]);
       }
+    }
   }
   // l over all keys since begin(), in every lane of its column
   __device__ __forceinline__ void end() {
 #pragma unroll
     for (int t = 0; t < QT; ++t) run.l[t] = bad ? __builtin_nanf("") : column_sum(run.l[t]);
+  }
+  // After end(): whether a sum is NaN though its weights are not, as infinite or NaN values make it.  Only then is a piece taken
+  // again with them apart: the check costs 0.1 us of a call, taking them apart at once would cost every step.
+  __device__ __forceinline__ bool spoiled() const {
+    bool nan = false;
+#pragma unroll
+    for (int t = 0; t < QT; ++t) {
+      f32x4 c[2] = {run.o[t][0], run.o[t][1]};  // NaN where one of its terms is
+#pragma unroll
+      for (int i = 2; i < VC; ++i) c[i % 2] += run.o[t][i];
+      c[0] += c[1];
+      nan |= __builtin_isnan((c[0][0] + c[0][1]) + (c[0][2] + c[0][3])) && !__builtin_isnan(run.l[t]);
+    }
+    return __any(nan);
+  }
+  // One step by itself, with infinite and NaN values apart.
+  __device__ __forceinline__ void step_apart(const int32_t* pt, int len, int s, int kvh) {
+    bool outside;
+    const int2 ids = usable(step_pages(pt, a.max_pages, s), len, s, outside);
+    bad |= outside;
+    load_k(ids, kvh);
+    load_v(v_at(ids, kvh));
+    float p[QT][8];
+    scores(p);
+    weigh<true>(p, len - kStep * s);
   }
 };
 
@@ -289,10 +341,12 @@ __device__ __forceinline__ void store4(bf16_t* p, const f32x4& v, float r) {
   *reinterpret_cast<uint2*>(p) = make_uint2(h[0] | (uint32_t)h[1] << 16, h[2] | (uint32_t)h[3] << 16);
 }
 
-// Adds parts first, first + step, ... (N of them) by the whole workgroup.
+// Adds parts first, first + step, ... (N of them) by the whole workgroup.  True where an output is NaN though its weights are
+// not, as infinite or NaN values make it.
 template <int HD, CacheType T, int N>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, int env, const HeadBlock& b, const Parts<HD>& ps, int first,
+__device__ __forceinline__ bool join_parts(const PagedAttnArgs& a, int env, const HeadBlock& b, const Parts<HD>& ps, int first,
                                            int n, int second, int step, const Partial& to) {
+  bool spoiled = false;
   for (int i = threadIdx.x; i < b.n * (HD / 4); i += blockDim.x) {
     const int h = i / (HD / 4), f = 4 * (i % (HD / 4));
     float mu[N], m = -INFINITY, l = 0.f;
@@ -307,7 +361,7 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, int env, cons
     for (int u = 0; u < N; ++u) {
       if (u >= n) break;
       const int p = u == 0 ? first : second + (u - 1) * step;
-      const float c = mu[u] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mu[u] - m);  // a part without keys adds zeros
+      const float c = mu[u] == -INFINITY ? 1.f : worth(mu[u], m);  // a part without keys adds zeros
       l = fmaf(ps.ml[(p * 2 + 1) * ps.rows + h], c, l);
       const f32x4 o = *reinterpret_cast<const f32x4*>(ps.o + (size_t)(p * ps.rows + h) * (HD + 4) + f);
 #pragma unroll
@@ -322,8 +376,10 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, int env, cons
     } else {
       store4<T>(a.o + env * a.ld_o + (size_t)(b.head0 + h) * HD + f, v, reciprocal(l));
       if (a.lse && f == 0) a.lse[(size_t)env * a.n_heads + b.head0 + h] = log_sum<T>(m, l);
+      spoiled |= __builtin_isnan((v[0] + v[1]) + (v[2] + v[3])) && !__builtin_isnan(l);
     }
   }
+  return spoiled;
 }
 
 // An environment's number of steps; 0 for one that gets zeros or NaN.
@@ -345,6 +401,7 @@ __device__ __forceinline__ void no_keys(const PagedAttnArgs& a, int env, int hea
 template <int HD, CacheType T, int QT, bool STREAM, int W>
 __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a, int rows) {
   extern __shared__ __align__(16) float lds[];
+  __shared__ int again;
   const int env = blockIdx.y, len = __builtin_amdgcn_readfirstlane(a.lens[env]), steps = steps_of(a, len);
   const HeadBlock b = head_block<QT>(a, blockIdx.x);
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -373,12 +430,22 @@ __global__ __launch_bounds__(64 * W) void attn_whole_kernel(PagedAttnArgs a, int
         next_v = wave.v_at(ids, b.kvh);
         ids = step_pages(pt, a.max_pages, s + 2 * W);
       }
-      wave.weigh(p, len - kStep * s);
+      wave.template weigh<false>(p, len - kStep * s);
       if (more) wave.load_v(next_v);
     }
   }
   wave.end();
   Parts<HD> ps(lds, W, rows);
+  ps.put(w, wave.run, b.n);
+  if (threadIdx.x == 0) again = 0;
+  __syncthreads();
+  if (join_parts<HD, T, W>(a, env, b, ps, 0, W, 1, 1, {nullptr, nullptr, 0})) again = 1;
+  __syncthreads();
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(again) == 0, 1)) return;
+  wave.begin();  // once more with infinite and NaN values apart; the queries are still there
+#pragma nounroll
+  for (int s = w; s < steps; s += W) wave.step_apart(pt, len, s, b.kvh);
+  wave.end();
   ps.put(w, wave.run, b.n);
   __syncthreads();
   join_parts<HD, T, W>(a, env, b, ps, 0, W, 1, 1, {nullptr, nullptr, 0});
@@ -487,9 +554,29 @@ __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, 
     Place cur = {env0, 0, 0, len_0, steps_of(a, len_0)};
     cur.hb = into / (unsigned)cur.steps;
     cur.s = into - cur.hb * cur.steps;
+    const int s0 = cur.s;
     bool began = cur.s == 0, outside;  // whether the piece began in this run
+    int left = 0;  // steps of the run from a spoiled piece on
     HeadBlock b = head_block<QT>(a, cur.hb);
     Wave<HD, T, QT, STREAM> wave(a);
+    // What the run holds of a piece up to p, its last step in the run: all of it to the output, or a part to LDS.
+    auto all_of = [&](const Place& p, bool began) { return began && p.s == p.steps - 1; };
+    auto write = [&](const Place& p, const HeadBlock& b) {
+      const int m16 = lane & 15, g = lane >> 4;
+#pragma unroll
+      for (int t = 0; t < QT; ++t)
+        if (16 * t + m16 < b.n) {
+          bf16_t* o = a.o + p.env * a.ld_o + (size_t)(b.head0 + 16 * t + m16) * HD + 4 * g;
+          const float r = reciprocal(wave.run.l[t]);
+#pragma unroll
+          for (int j = 0; j < HD / 16; ++j) store4<T>(o + 16 * j, wave.run.o[t][j], r);
+          if (a.lse && g == 0) a.lse[(size_t)p.env * a.n_heads + b.head0 + 16 * t + m16] = log_sum<T>(wave.run.m[t], wave.run.l[t]);
+        }
+    };
+    auto keep = [&](const Place& p, const HeadBlock& b, bool began) {
+      ps.put(2 * w + began, wave.run, b.n);
+      if (lane == 0) ends[w][began] = make_int4(p.env, p.hb, p.steps - 1 - p.s, 1);
+    };
     wave.begin();
     int2 ids = step_pages(table + cur.env * a.ld_table, a.max_pages, cur.s);
     wave.load_q(cur.env, b);
@@ -522,26 +609,18 @@ __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, 
           ids = step_pages(table + third.env * a.ld_table, a.max_pages, third.s);
         }
       }
-      wave.weigh(p, cur.len - kStep * cur.s);
+      wave.template weigh<false>(p, cur.len - kStep * cur.s);
       if (more) wave.load_v(next_v);
       if (ends_here) {
         wave.end();
-        const int past = cur.steps - 1 - cur.s;  // steps of the piece after this run
-        if (began && past == 0) {
-          const int m16 = lane & 15, g = lane >> 4;
-#pragma unroll
-          for (int t = 0; t < QT; ++t)
-            if (16 * t + m16 < b.n) {
-              bf16_t* o = a.o + cur.env * a.ld_o + (size_t)(b.head0 + 16 * t + m16) * HD + 4 * g;
-              const float r = reciprocal(wave.run.l[t]);
-#pragma unroll
-              for (int j = 0; j < HD / 16; ++j) store4<T>(o + 16 * j, wave.run.o[t][j], r);
-              if (a.lse && g == 0) a.lse[(size_t)cur.env * a.n_heads + b.head0 + 16 * t + m16] = log_sum<T>(wave.run.m[t], wave.run.l[t]);
-            }
-        } else {
-          ps.put(2 * w + began, wave.run, b.n);
-          if (lane == 0) ends[w][began] = make_int4(cur.env, cur.hb, past, 1);
+        const bool all = all_of(cur, began);
+        if (!all) keep(cur, b, began);  // its writes go on while the sums are looked at
+        if (__builtin_expect(wave.spoiled(), 0)) {
+          left = n - i + cur.s - (began ? 0 : s0);
+          cur.s = began ? 0 : s0;
+          break;
         }
+        if (all) write(cur, b);
         if (more) {
           wave.begin();
           began = true;
@@ -551,6 +630,27 @@ __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, 
       cur = next;
       next = third;
       b = nb;
+    }
+    if (__builtin_expect(left > 0, 0)) {  // that piece once more and the others after it
+      bool first = true;
+#pragma nounroll
+      do {
+        b = head_block<QT>(a, cur.hb);
+        if (first || cur.s == 0) {
+          wave.begin();
+          wave.load_q(cur.env, b);
+        }
+        first = false;
+        wave.step_apart(table + cur.env * a.ld_table, cur.len, cur.s, b.kvh);
+        next = --left > 0 ? after(a, lens, cur, blocks) : cur;
+        if (left == 0 || next.s == 0) {
+          wave.end();
+          if (all_of(cur, began)) write(cur, b);
+          else keep(cur, b, began);
+          began = true;
+        }
+        cur = next;
+      } while (left > 0);
     }
   }
   __syncthreads();
@@ -625,7 +725,7 @@ __device__ __forceinline__ void join_piece(const PagedAttnArgs& a, const SplitSp
   for (int i = 0; i < NW; ++i) m = fmaxf(m, sm[i]);
 #pragma unroll
   for (int j = 0; j < PT; ++j) {
-    const float c = mp[j] == -INFINITY ? 1.f : __builtin_amdgcn_exp2f(mp[j] - m);
+    const float c = mp[j] == -INFINITY ? 1.f : worth(mp[j], m);
     sc[tid + j * kJoinThreads] = c;
     l = fmaf(lp[j], c, l);
   }

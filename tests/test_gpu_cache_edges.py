@@ -62,3 +62,76 @@ def test_heads_without_a_score_are_zeros_whatever_the_values(lens, H, K, hd, ext
     if K > 1:
         even = np.arange(K) % 2 == 0
         check_attention(got[:, ~odd], lse[:, ~odd], q[:, ~odd], kp[:, even], vp[:, even], table, lens, hd ** -0.5)
+
+
+def check_with_infinities(got, lse, q, kp, vp, table, lens, scale):
+    """NaN and infinities where the 64-bit sums have them, all else within the tolerance; log-sum-exp as ever."""
+    n, H, hd = q.shape
+    with np.errstate(invalid="ignore"):
+        ref, rlse, mag, smax = co.paged_attention(f64(q), f64(kp), f64(vp), table, lens, scale)
+    g, fin = f64(got), np.isfinite(ref)
+    assert np.array_equal(np.isnan(g), np.isnan(ref)), np.argwhere(np.isnan(g) != np.isnan(ref))[:5]
+    inf = np.isinf(ref)
+    assert np.array_equal(g[inf], ref[inf]) and inf.any()
+    tol = attn_tol(np.where(fin, ref, 0), np.where(fin, mag, 0), smax, hd, got.dtype)
+    assert np.all(np.abs(g - np.where(fin, ref, 0))[fin] <= tol[fin])
+    one = np.isfinite(rlse)
+    assert np.all(np.abs(f64(lse) - np.where(one, rlse, 0))[one] <= (2 * (hd + 32) * 2.0 ** -24 * np.maximum(smax, 1) +
+                                                                       4 * 2.0 ** -24 * np.abs(np.where(one, rlse, 0)))[one])
+
+
+def spread_infinities(vp, table, lens, seed):
+    """In every environment and key head: feature 0 has one infinity, 1 one of the other sign, 2 three of one sign, 3 both
+    signs, 4 a NaN beside one, 5 one at the last token; all others are finite."""
+    rng = np.random.default_rng(seed)
+    put = {math.inf: [], -math.inf: [], math.nan: []}
+    for e, n in enumerate(lens):
+        for h in range(vp.shape[1] if n > 0 else 0):
+            sign = rng.choice([math.inf, -math.inf])
+            where = [(0, sign, rng.integers(n)), (1, -sign, rng.integers(n)), (5, sign, n - 1), (4, math.nan, rng.integers(n))]
+            where += [(2, sign, t) for t in rng.integers(0, n, 3)]
+            if n > 1:
+                a, b = rng.choice(n, 2, replace=False)
+                where += [(3, sign, a), (3, -sign, b)]
+                where += [(4, sign, a)] if where[3][2] != a else []
+            for f, x, t in where:
+                put[x].append((table[e, t // PAGE], h, f, t % PAGE))
+    for x, at in put.items():
+        vp[tuple(torch.from_numpy(c) for c in np.array(at).T)] = x
+
+
+@pytest.mark.parametrize("equal", [False, True])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("lens,H,K,hd,extra_cols", PATHS)
+def test_infinite_values_are_infinite_sums(lens, H, K, hd, extra_cols, dtype, equal):
+    """With weights that the type holds exactly (equal scores) and others."""
+    kp, vp, table, lens = make_cache(lens, K, hd, dtype, 5, extra_cols=extra_cols)
+    spread_infinities(vp, table, lens, 6)
+    q = rand((len(lens), H, hd), dtype, 7, 0.0 if equal else 2.0)
+    lse = torch.empty(len(lens), H, device="cuda")
+    got = vla.paged_attention(q, kp, vp, i32(table), i32(lens), hd ** -0.5, lse=lse)
+    check_with_infinities(got, lse, q, kp, vp, table, lens, hd ** -0.5)
+    again = vla.paged_attention(q, kp, vp, i32(table), i32(lens), hd ** -0.5)
+    assert torch.equal(got.nan_to_num(), again.nan_to_num())
+
+
+@pytest.mark.parametrize("below", [20.0, 60.0, 200.0])
+@pytest.mark.parametrize("dtype", [BF, FP])
+@pytest.mark.parametrize("first", [True, False])
+@pytest.mark.parametrize("n,extra_cols", [(90, 1), (2000, 1), (90, 80)])
+def test_infinite_values_of_weak_keys(n, extra_cols, first, dtype, below):
+    """A weight that no narrow type holds is a weight: infinities at keys far below the strongest, which comes before or after
+    them.  (Weights are above 0 in 64 bits up to about 700 below.)"""
+    hd = 64
+    kp, vp, table, lens = make_cache([n, n], 1, hd, dtype, 8, extra_cols=extra_cols)
+    q = torch.zeros(2, 1, hd, dtype=dtype, device="cuda")
+    q[..., 0] = below
+    kp[..., 0] = 0.0
+    strong, weak = (n - 1, 1) if first else (1, n - 1)
+    kp[table[0, strong // PAGE], 0, strong % PAGE, 0] = 1.0
+    vp[table[0, weak // PAGE], 0, 3, weak % PAGE] = -math.inf
+    vp[table[0, 2], 0, 9, 5] = math.inf
+    vp[table[1, 3], 0, 9, 5] = math.inf
+    lse = torch.empty(2, 1, device="cuda")
+    got = vla.paged_attention(q, kp, vp, i32(table), i32(lens), 1.0, lse=lse)
+    check_with_infinities(got, lse, q, kp, vp, table, lens, 1.0)
