@@ -520,7 +520,7 @@ __global__ __launch_bounds__(kRunThreads) void attn_run_kernel(PagedAttnArgs a, 
   extern __shared__ __align__(16) float lds[];
   __shared__ int4 ends[kRunWaves][2];  // per wave and part: environment, head block, steps past the run, valid
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), me = blockIdx.x;
-  if (lane < 2) ends[w][lane] = make_int4(0, 0, 0, 0);
+  if (lane == 0) ends[w][0] = ends[w][1] = make_int4(0, 0, 0, 0);  // by the lane that notes parts down later
   // every wave adds up the steps of all environments, each lane those of a run of them, and finds its place in the line
   const int per = (a.n_env + kWave - 1) / kWave, e0 = min(a.n_env, lane * per), e1 = min(a.n_env, e0 + per);
   const int len0 = e0 < e1 ? lens[e0] : 0;
