@@ -124,7 +124,8 @@ int vla_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor,
  * new key and v [rows, n_kv_heads, head_dim] go to slot row_slot[row]; a row
  * whose slot lies outside [0, 16 n_pages) is passed over: neither the cache
  * nor its rows of q_out and k_out are written.  Slots are distinct.
- * rows == 0 is a no-op. */
+ * rows == 0 is a no-op.  At most 2^26 - 4 rows; with a cache ceil(rows / 4) +
+ * ceil(rows / 16) ceil(n_kv_heads head_dim / 256) must be below 2^24. */
 #define VLA_ROPE_HALF 0
 #define VLA_ROPE_INTERLEAVED 1
 int vla_qk_norm_rope(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,

@@ -50,6 +50,8 @@ struct QkRopeArgs {
   int n_pages;
   const int32_t* row_slot;     // [rows] with pages
 };
+// Whether one launch takes that many rows: its threads have to stay below 2^32.
+bool qk_rope_fits(int rows, int n_heads, int n_kv_heads, int head_dim, bool cache);
 hipError_t launch_qk_rope(const QkRopeArgs& a, hipStream_t s);
 
 struct QkRopeBwdArgs {

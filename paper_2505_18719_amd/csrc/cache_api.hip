@@ -137,6 +137,7 @@ int vla_qk_norm_rope(int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t 
   if ((v != nullptr) != cache || (v_pages != nullptr) != cache || (row_slot != nullptr) != cache)
     return set_error(VLA_EINVAL, "v, k_pages, v_pages and row_slot go together");
   if (!cache && !k_out) return set_error(VLA_EINVAL, "k has nowhere to go: no k_out and no cache");
+  if (!qk_rope_fits(rows, n_heads, n_kv_heads, head_dim, cache)) return set_error(VLA_EUNSUPPORTED, "too many rows for one call");
   if ((rc = check_rows("q", q, ld_q, wq)) || (rc = check_rows("k", k, ld_k, wk)) ||
       (rc = check_rows("q_out", q_out, ld_qo, wq)) || (k_out && (rc = check_rows("k_out", k_out, ld_ko, wk))) ||
       (cache && (rc = check_rows("v", v, ld_v, wk))))

@@ -461,19 +461,31 @@ bool whole_lines(int rot_dim) {
   return HD >= 128 && (LAYOUT == 1 || rot_dim == HD || rot_dim == 0);
 }
 
+// The forward's launch: workgroups for queries and keys, `parts` waves a row, then those for tiles of values.
+struct FwdGrid {
+  int parts, tile;
+  long long groups, all;
+};
+FwdGrid fwd_grid(int rows, int n_heads, int n_kv_heads, int head_dim, bool cache) {
+  const int per_wave = kWave / (head_dim / 16), heads = n_heads + n_kv_heads;
+  FwdGrid g;
+  g.parts = rows >= 2048 ? 1 : (heads + per_wave - 1) / per_wave;
+  g.tile = std::min(kTileRows, std::max(1, rows / 512));
+  g.groups = ((long long)rows * g.parts + kRopeWaves - 1) / kRopeWaves;
+  const long long tiles = (rows - 1) / g.tile + 1, quads = cache ? (n_kv_heads * (head_dim / kSlice) + kRopeWaves - 1) / kRopeWaves : 0;
+  g.all = g.groups + tiles * quads;
+  return g;
+}
+
 template <int HD, CacheType T, int LAYOUT>
 struct Fwd {
   static hipError_t run(const QkRopeArgs& a, hipStream_t s) {
-    constexpr int HPW = kWave / (HD / 16);
-    const int heads = a.n_heads + a.n_kv_heads, parts = a.rows >= 2048 ? 1 : (heads + HPW - 1) / HPW;
-    const long long groups = ((long long)a.rows * parts + kRopeWaves - 1) / kRopeWaves;
-    const int tile = std::min(kTileRows, std::max(1, a.rows / 512));
-    const long long tiles = (a.rows - 1) / tile + 1, quads = a.pages.v ? (a.n_kv_heads * (HD / kSlice) + kRopeWaves - 1) / kRopeWaves : 0;
-    if (groups + tiles * quads > 0x7fffffffll) return hipErrorInvalidValue;
-    const dim3 grid((unsigned)(groups + tiles * quads)), block(kRopeThreads);
-    const bool stream = whole_lines<HD, LAYOUT>(a.rot_dim) && (size_t)a.rows * (heads + a.n_kv_heads) * HD * 4 > kStreamBytes;
-    if (stream) hipLaunchKernelGGL((qk_rope_kernel<HD, T, LAYOUT, true>), grid, block, 0, s, a, (int)groups, parts, tile);
-    else hipLaunchKernelGGL((qk_rope_kernel<HD, T, LAYOUT, false>), grid, block, 0, s, a, (int)groups, parts, tile);
+    const FwdGrid g = fwd_grid(a.rows, a.n_heads, a.n_kv_heads, HD, a.pages.v != nullptr);
+    const dim3 grid((unsigned)g.all), block(kRopeThreads);
+    const size_t bytes = (size_t)a.rows * (a.n_heads + 2 * a.n_kv_heads) * HD * 4;
+    const bool stream = whole_lines<HD, LAYOUT>(a.rot_dim) && bytes > kStreamBytes;
+    if (stream) hipLaunchKernelGGL((qk_rope_kernel<HD, T, LAYOUT, true>), grid, block, 0, s, a, (int)g.groups, g.parts, g.tile);
+    else hipLaunchKernelGGL((qk_rope_kernel<HD, T, LAYOUT, false>), grid, block, 0, s, a, (int)g.groups, g.parts, g.tile);
     return hipGetLastError();
   }
 };
@@ -514,6 +526,9 @@ hipError_t by_head(const A& a, hipStream_t s) {
 
 }  // namespace
 
+bool qk_rope_fits(int rows, int n_heads, int n_kv_heads, int head_dim, bool cache) {
+  return fwd_grid(rows, n_heads, n_kv_heads, head_dim, cache).all * kRopeThreads < 1ll << 32;
+}
 size_t qk_rope_bwd_floats(int head_dim) { return (size_t)kBwdGroups * 2 * head_dim; }
 hipError_t launch_qk_rope(const QkRopeArgs& a, hipStream_t s) { return by_head<Fwd>(a, s); }
 hipError_t launch_qk_rope_bwd(const QkRopeBwdArgs& a, hipStream_t s) { return by_head<Bwd>(a, s); }

@@ -135,3 +135,21 @@ def test_infinite_values_of_weak_keys(n, extra_cols, first, dtype, below):
     lse = torch.empty(2, 1, device="cuda")
     got = vla.paged_attention(q, kp, vp, i32(table), i32(lens), 1.0, lse=lse)
     check_with_infinities(got, lse, q, kp, vp, table, lens, 1.0)
+
+
+# ------------------------------------------------------------------ the largest calls
+def test_norm_rope_of_the_most_rows():
+    """2^26 - 4 rows, the most that one call takes: rows of the ends and beyond 2^32 bytes as in a call of their own."""
+    rows, hd = 2 ** 26 - 4, 64
+    pick = torch.tensor([0, 1, 2, 3, 2 ** 25 - 1, 2 ** 25, 2 ** 25 + 1, 2 ** 26 - 2 ** 13, rows - 5, rows - 2, rows - 1],
+                        device="cuda")
+    q = torch.zeros(rows, 1, hd, dtype=BF, device="cuda")
+    k = torch.zeros(rows, 1, hd, dtype=BF, device="cuda")
+    pos = torch.arange(rows, dtype=torch.int32, device="cuda")
+    q[pick], k[pick] = rand((len(pick), 1, hd), BF, 1), rand((len(pick), 1, hd), BF, 2)
+    f = vla.rope_freqs(hd)[0]
+    want = vla.qk_norm_rope(q[pick], k[pick], pos[pick], f)
+    vla.qk_norm_rope(q, k, pos, f, q_out=q, k_out=k)
+    assert torch.equal(q[pick], want[0]) and torch.equal(k[pick], want[1])
+    q[pick], k[pick] = 0, 0
+    assert not q.any() and not k.any()
