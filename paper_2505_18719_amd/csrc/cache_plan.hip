@@ -64,10 +64,11 @@ __global__ __launch_bounds__(NT) void kv_plan_kernel(KvPlanArgs a, int rows_per_
   const unsigned avail = head >= 0 && head <= a.n_free ? a.n_free - head : 0;
   unsigned row = 0, page = 0, taken = 0;  // rows and pages asked for before the tile; pages given out
   int refused = 0;
-  for (int t0 = 0; t0 < a.n_env; t0 += NT) {
+  const unsigned n_env = a.n_env;  // the last tile may end past 2^31 - 1
+  for (unsigned t0 = 0; t0 < n_env; t0 += NT) {
     if (!first && row >= r1) break;
-    const int e = t0 + tid;
-    const bool in = e < a.n_env;
+    const unsigned e = t0 + tid;
+    const bool in = e < n_env;
     const int c = in ? a.cached[e] : 0, w = in ? a.added[e] : 0;
     unsigned tile_rows, tile_pages;
     const unsigned rows = max(w, 0), end = add_sat(row, block_scan<W>(rows, sums[0], tile_rows));
@@ -103,7 +104,7 @@ __global__ __launch_bounds__(NT) void kv_plan_kernel(KvPlanArgs a, int rows_per_
         if (p >= 0 && p < a.n_pages) slot = p * kPage + (int)(pos % kPage);
       }
       a.row_pos[r] = (int)min(max(pos, 0ll), 0x7fffffffll);
-      a.row_env[r] = t0 + i;
+      a.row_env[r] = (int)(t0 + i);
       a.row_slot[r] = slot;
     }
     row = add_sat(row, tile_rows);

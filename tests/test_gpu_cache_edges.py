@@ -153,3 +153,14 @@ def test_norm_rope_of_the_most_rows():
     assert torch.equal(q[pick], want[0]) and torch.equal(k[pick], want[1])
     q[pick], k[pick] = 0, 0
     assert not q.any() and not k.any()
+
+
+def test_plan_of_the_most_environments():
+    """2^31 - 1 environments, one tile of which ends past that: only the last one has a row, which no page takes."""
+    n = 2 ** 31 - 1
+    cached, new = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda")
+    new[-1] = 1
+    out = vla.kv_plan(cached, new, torch.empty(n, 0, dtype=torch.int32, device="cuda"), i32([7]), 8, 3)
+    assert out["stats"].tolist() == [0, 1, 1]
+    assert out["row_env"].tolist() == [n - 1, -1, -1] and out["row_slot"].tolist() == [-1] * 3 and out["row_pos"].tolist() == [0] * 3
+    assert int(out["row_start"][-1]) == 1 and not out["row_start"][:-1].any() and not out["lens"].any()
