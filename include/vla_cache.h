@@ -175,6 +175,7 @@ int vla_qk_norm_rope_backward(int32_t rows, int32_t n_heads, int32_t n_kv_heads,
  *                may share pages.  The work is laid out for lengths up to 16 *
  *                max_pages, so pass no more columns than the step needs
  *   lens         int32 [n_env] (vla_kv_plan's)
+ *   scale        finite, at most 2.3e38 in size (softmax is taken to base 2)
  *   lse          fp32 [n_env, n_heads] out, or NULL: log sum_j exp(scale q . k_j)
  *                (-inf where the output is zeros for want of a key)
  *   workspace    vla_paged_attention_workspace_size bytes, 256-byte aligned

@@ -229,7 +229,7 @@ int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int3
   if (rc != VLA_OK) return rc;
   if (n_pages < 0) return set_error(VLA_EINVAL, "negative size");
   if (n_pages >= 1 << 27) return set_error(VLA_EUNSUPPORTED, "n_pages must be below 2^27");
-  if (!std::isfinite(scale)) return set_error(VLA_EINVAL, "scale must be finite");
+  if (!std::isfinite(scale * 1.44269504f)) return set_error(VLA_EINVAL, "scale must be finite, times log2(e) too");
   if (n_env == 0) return set_error(VLA_OK, "");
   const int64_t width = (int64_t)n_heads * head_dim;
   if ((rc = check_rows("q", q, ld_q, width)) || (rc = check_rows("out", out, ld_o, width))) return rc;

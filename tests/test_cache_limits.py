@@ -43,3 +43,9 @@ def test_norm_rope_refuses_more_rows_than_a_launch_takes(lib, kv, hd, cache):
         rc = lib.vla_qk_norm_rope(rows, kv, kv, hd, 0, P, w, P, w, c[0], c[1], None, None, 1e-6, P, P, 64, 0, 1.0, 2 * P, w,
                                   2 * P, w, c[2], c[3], c[4], c[5], None)
         assert rc == -7 and b"rows" in lib.vla_last_error(), (rows, rc)
+
+
+@pytest.mark.parametrize("scale", [2.4e38, -3.4e38])
+def test_attention_refuses_a_scale_without_room_for_base_2(lib, scale):
+    rc = lib.vla_paged_attention(4, 8, 2, 128, 0, P, 1024, P, P, 9, P, 8, 8, P, scale, 2 * P, 1024, None, P, 1 << 40, None)
+    assert rc == -1 and b"scale" in lib.vla_last_error()
