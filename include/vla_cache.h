@@ -84,7 +84,7 @@ int vla_kv_plan(int32_t n_env, const int32_t* cached_lens, const int32_t* new_le
  *   VLA_ROPE_LINEAR  f_i / factor: positions interpolated
  *   VLA_ROPE_BASE    base times factor^(rot_dim / (rot_dim - 2)), which
  *                    divides the lowest frequency by factor and leaves the
- *                    highest (rot_dim >= 4)
+ *                    highest (rot_dim >= 4, the new base finite)
  *   VLA_ROPE_BANDS   by turns over the trained context, n_i = context f_i /
  *                    (2 pi): f_i from `high` turns on, f_i / factor up to
  *                    `low`, between them f_i (w + (1 - w) / factor) with w =

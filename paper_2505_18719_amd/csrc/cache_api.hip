@@ -96,6 +96,7 @@ int vla_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor,
   constexpr double kTwoPi = 6.283185307179586476925;
   const double d = rot_dim;
   if (scaling == VLA_ROPE_BASE) base *= std::pow(factor, d / (d - 2));
+  if (!std::isfinite(base)) return set_error(VLA_EINVAL, "the changed base must be finite");
   double a = 0, b = 0;
   if (scaling == VLA_ROPE_RAMP) {
     auto index = [&](double turns) { return d / 2 * std::log(context / (kTwoPi * turns)) / std::log(base); };

@@ -49,3 +49,9 @@ def test_norm_rope_refuses_more_rows_than_a_launch_takes(lib, kv, hd, cache):
 def test_attention_refuses_a_scale_without_room_for_base_2(lib, scale):
     rc = lib.vla_paged_attention(4, 8, 2, 128, 0, P, 1024, P, P, 9, P, 8, 8, P, scale, 2 * P, 1024, None, P, 1 << 40, None)
     assert rc == -1 and b"scale" in lib.vla_last_error()
+
+
+@pytest.mark.parametrize("rot,base,factor", [(64, 1e300, 1e9), (4, 1e4, 1e160)])
+def test_rope_freqs_refuses_a_changed_base_past_64_bits(lib, rot, base, factor):
+    buf = (ctypes.c_double * 256)()
+    assert lib.vla_rope_freqs(rot, base, 2, factor, 1.0, 4.0, 8192.0, buf, None) == -1 and b"base" in lib.vla_last_error()
