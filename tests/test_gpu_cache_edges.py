@@ -164,3 +164,21 @@ def test_plan_of_the_most_environments():
     assert out["stats"].tolist() == [0, 1, 1]
     assert out["row_env"].tolist() == [n - 1, -1, -1] and out["row_slot"].tolist() == [-1] * 3 and out["row_pos"].tolist() == [0] * 3
     assert int(out["row_start"][-1]) == 1 and not out["row_start"][:-1].any() and not out["lens"].any()
+
+
+# ------------------------------------------------------------------ appends
+@pytest.mark.parametrize("dtype,K,hd", [(BF, 3, 64), (FP, 2, 128), (BF, 1, 256)])
+@pytest.mark.parametrize("rows,runs", [(1, False), (37, True), (129, False), (600, True)])
+def test_appends_without_norm_and_rotation_are_copies(rows, runs, dtype, K, hd):
+    """Keys and values as they are, infinities and NaN among them, at runs of slots and at scattered ones; rows with slots
+    outside the pool are passed over."""
+    rng = np.random.default_rng(rows)
+    n_pages = rows // PAGE + 4
+    slots = np.arange(rows) + 5 if runs else rng.permutation(n_pages * PAGE)[:rows]
+    slots[rng.permutation(rows)[:rows // 9]] = rng.choice([-1, -2 ** 31, n_pages * PAGE, 2 ** 31 - 1], rows // 9)
+    q, k, v = rand((rows, K, hd), dtype, 1), rand((rows, K, hd), dtype, 2), rand((rows, K, hd), dtype, 3)
+    k[0, 0, :3] = v[rows // 2, 0, :3] = torch.tensor([math.inf, -math.inf, math.nan], device="cuda")
+    kp, vp = rand((n_pages, K, PAGE, hd), dtype, 4), rand((n_pages, K, hd, PAGE), dtype, 5)
+    want = co.append(f64(kp), f64(vp), slots, f64(k), f64(v))
+    vla.qk_norm_rope(q, k, None, None, v=v, k_pages=kp, v_pages=vp, row_slot=i32(slots))
+    assert np.array_equal(f64(kp), want[0], equal_nan=True) and np.array_equal(f64(vp), want[1], equal_nan=True)
