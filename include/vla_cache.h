@@ -28,10 +28,12 @@
  * number `slot` is 16 * page + p % 16.  n_pages < 2^27.
  *
  * `dtype` is the type of q, k, v, gains, pages and outputs.  Sums, softmax
- * statistics and rotation angles are held in 32 bits or more and each output
- * is rounded once, to nearest even.  Tensors start on 16 bytes; a row holds its
- * heads contiguously, and row strides (`ld_*`, in elements) are multiples of
- * 8 that hold a row, so q, k and v may be parts of one projection's output.
+ * statistics and rotation angles are held in 32 bits or more, and each output
+ * is rounded once, to nearest even; softmax weights meet the values as pairs of
+ * numbers of `dtype` (16 bits in bf16, 22 in fp16).  Tensors of `dtype` and fp64
+ * start on 16 bytes, others on 4; a row holds its heads contiguously, and row
+ * strides (`ld_*`, in elements) are multiples of 8 that hold a row, so q, k and
+ * v may be parts of one projection's output.
  * At most 1024 heads and 1024 key heads.
  */
 #ifndef VLA_CACHE_H_
@@ -106,7 +108,8 @@ int vla_rope_freqs(int32_t rot_dim, double base, int32_t scaling, double factor,
 
 /* Norms of q and k per head and their rotation, in one pass, with the append
  * to the cache.  For each row at position p = row_pos[row] and each head,
- *     y = x gain / sqrt(mean(x^2) + eps)      (y = x where the gain is NULL)
+ *     y = x gain / sqrt(mean(x^2) + eps)      (y = x where the gain is NULL;
+ * the sum of the squares is fp32's: past 3.4e38 the head becomes zeros)
  * then, with (a, b) the pair i of y's first rot_dim features, t = p freqs[i]
  * (taken in 64 bits) and s = rope_scale,
  *     (a, b) -> (s (a cos t - b sin t), s (b cos t + a sin t));
@@ -173,7 +176,9 @@ int vla_qk_norm_rope_backward(int32_t rows, int32_t n_heads, int32_t n_kv_heads,
  *                64, 128 or 256; n_heads a multiple of n_kv_heads
  *   page_table   int32 [n_env, max_pages] (row stride ld_table); environments
  *                may share pages.  The work is laid out for lengths up to 16 *
- *                max_pages, so pass no more columns than the step needs
+ *                max_pages: columns that no length needs cost some time (where
+ *                lengths are not known beforehand, as in a graph, they are the
+ *                price) and change no result by more than its rounding
  *   lens         int32 [n_env] (vla_kv_plan's)
  *   scale        finite, at most 2.3e38 in size (softmax is taken to base 2)
  *   lse          fp32 [n_env, n_heads] out, or NULL: log sum_j exp(scale q . k_j)

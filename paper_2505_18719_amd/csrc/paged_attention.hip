@@ -823,10 +823,11 @@ hipError_t launch_run(const PagedAttnArgs& a, int blocks, int rows, hipStream_t 
 }
 
 // Whether the keys are split, of `pieces` environments and head blocks.  Short keys are taken whole: the split's second launch
-// and its way through the workspace cost more than they save (GPU us, whole / split: 1 x 278 tokens, 32 pieces, 6.2 / 10; 1 x
-// 512, 8 pieces, 7.5 / 9.1), up to 1024 tokens where there are pieces enough to fill half the GPU (32 x 700 tokens, 256 pieces,
-// 17.9 / 25.6; 16 of up to 1024, 128 pieces, 12.7 / 15.1; but 8 x 1024, 64 pieces, 18 / 14.3).  Beyond, the split is as fast where
-// pieces abound and faster where they are few or uneven (1 x 1024 16.9 / 9.3; 64 of up to 2048 53.8 / 52.7).
+// and its way through the workspace cost more than they save (GPU us, whole / split: 1 x 278 tokens, 32 pieces, 6.3 / 10.5; 1 x
+// 512, 8 pieces, 7.6 / 9.5), up to 1024 tokens where there are pieces enough to fill half the GPU (32 x 700 tokens, 256 pieces,
+// 18.2 / 26.1; 16 of up to 1024, 128 pieces, 12.8 / 15.3; but 8 x 1024, 64 pieces, 18.2 / 14.5).  Beyond, the split is about as
+// fast where pieces abound (64 x 4096, 512 pieces, 169 / 172.5) and faster where they are few or uneven (1 x 1024, 8 pieces, 12.0 /
+// 9.8; 8 x 3000, 8 pieces, 29.6 / 11.4; 64 of up to 2048 56.5 / 54.0).
 bool split_keys(long long pieces, int max_pages) { return max_pages > (pieces >= 128 ? 64 : 32); }
 
 template <int HD, CacheType T, int QT, bool STREAM>
@@ -844,8 +845,8 @@ hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
 // not fit), further ones read the keys again.
 int query_tiles(int group, int head_dim) { return head_dim < 256 && group > 16 ? 2 : 1; }
 
-// A pool of up to 32 MB, the L2s' size, may be in the caches from one step to the next (278 tokens, 32 key heads: 6.2 us with
-// cached loads, 7.5 past the caches); beyond, reads past the caches are faster (64 x 4096: 191 and 173 us).
+// A pool of up to 32 MB, the L2s' size, may be in the caches from one step to the next (278 tokens, 32 key heads: 6.3 us with
+// cached loads; in a larger pool, past the caches, 7.9); beyond, reads past the caches are faster (64 x 4096: 191 and 173 us).
 bool stream_pool(const PagedAttnArgs& a) {
   return (size_t)a.n_pages * a.n_kv_heads * kPage * a.head_dim * 2 * sizeof(bf16_t) > (size_t)32 << 20;
 }

@@ -3,8 +3,9 @@
 //
 // Bound: HBM, every feature read once and written once (the gradient: two read, one written).  A head vector is held by
 // head_dim / 16 lanes, 16 features each, placed so that both features of every pair are in one lane: the norm is a sum over
-// 4, 8 or 16 lanes by DPP, the rotation needs no exchange.  Measured at 32 + 8 heads of 128: 18432 rows appended in 85 us, 453
-// MB, 5.3 TB/s (a copy of 1 GiB: 5.2); the gradient of 18880 rows 112 us, 580 MB, 5.2 TB/s; one row 3.1 us.
+// 4, 8 or 16 lanes by DPP, the rotation needs no exchange.  Measured at 32 + 8 heads of 128: 18432 rows appended in 82 us, 453
+// MB, 5.5 TB/s (a copy of 1 GiB past the caches, as these accesses are: 6.0); the gradient of 18880 rows 109 us and 5 for the
+// gains, 580 MB, 5.1 TB/s; one row 3.1 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>

@@ -579,7 +579,8 @@ def _table(t: torch.Tensor, index: int, n_env: int):
 
 def rope_freqs(rot_dim: int, base: float = 10000.0, scaling: str = "none", factor: float = 1.0, low: float = 1.0,
                high: float = 4.0, context: float = 8192, device="cuda"):
-    """(freqs fp64 [rot_dim / 2] on `device`, rope_scale) of a rotation (vla_rope_freqs)."""
+    """(freqs fp64 [rot_dim / 2] on `device`, rope_scale) of a rotation (vla_rope_freqs).  low and high default to the turns
+    that suit "bands"; "ramp" is usually given high=32."""
     lib = load_library()
     f = torch.empty(max(0, rot_dim // 2), dtype=torch.float64)
     scale = ctypes.c_float()
@@ -623,7 +624,7 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, row_pos: Optional[torch.Tenso
                  k_out: Optional[torch.Tensor] = None):
     """Head norms and rotation of q [rows, n_heads, head_dim] and k [rows, n_kv_heads, head_dim] (views of one projection's
     output will do), and with pages the append of k and v at row_slot (vla_qk_norm_rope).  Returns (q_out, k_out); with a
-    cache k_out is written only if it is passed in."""
+    cache k_out is written only if it is passed in.  Takes no part in autograd: its gradient is qk_norm_rope_backward."""
     lib = _lib or load_library()
     rows, H, hd, dt, index = _heads(q, "q")
     dtype, K = q.dtype, k.shape[1]
