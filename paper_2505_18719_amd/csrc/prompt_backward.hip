@@ -1,0 +1,332 @@
+// Gradient of causal attention over whole prompts (vla_prompt_attention_backward), in two passes that share nothing but D and the
+// log-sum-exps, so that no sum depends on the order of workgroups:
+//   queries: a wave holds 32 queries as MFMA columns, tiles of keys and values pass through LDS: S^T = K Q^T, dP^T = V dO^T - D,
+//            dQ^T += K^T dS^T
+//   keys:    a wave holds 32 keys as columns and goes over the queries behind them, of every head that reads the keys:
+//            S = Q K^T, dP = dO V^T - D, dV^T += dO^T P, dK^T += Q^T dS
+// Bound: the matrix units.  The gradient is 10 head_dim flops a query-key pair; scores and dP are computed in both passes, which
+// makes 14.  Each tile lies in LDS once, read by rows for one product and transposed for the other.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+
+#include "lds_limit.h"
+#include "prompt.h"
+#include "prompt_dev.h"
+
+namespace vla {
+namespace {
+
+// Of a query: its log-sum-exp to base 2 (+inf where it has no score above -inf: all weights 0), and D.
+struct RowStat {
+  float lse, d;
+};
+__device__ __forceinline__ float lse_base2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
+// Products with a column's weights, of any size, in the type's range.  In bf16 as they are.  Half precision has 5 bits of exponent:
+// each column's weights are held times a power of two that keeps the largest so far below 2^15 (and at first within a factor of four
+// of it), and what is summed follows when that changes.
+template <int HD, CacheType T>
+struct Column {
+  f32x16 sum[HD / 32];
+  float unit;
+  __device__ __forceinline__ void begin() {
+    unit = T == kBf16 ? 1.f : 0x1p120f;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) sum[i] = zeros16();
+  }
+  __device__ __forceinline__ void fit(f32x16& w) {
+    if constexpr (T == kF16) {
+      float mx = fabsf(w[0]);
+#pragma unroll
+      for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fabsf(w[r]));
+      mx = half_max(mx);
+      const bool grown = mx * unit > 0x1p15f && mx < INFINITY;
+      if (__any(grown)) {
+        const float u = grown ? ldexpf(1.f, min(max(14 - __builtin_amdgcn_frexp_expf(mx), -120), 120)) : unit;
+        const float c = u / unit;
+#pragma unroll
+        for (int i = 0; i < HD / 32; ++i) sum[i] *= c;
+        unit = u;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) w[r] *= unit;
+    }
+  }
+  // sum += x^T w over the 32 rows of a tile from 32 t on, w rounded to the type: a relative 2^-9 (2^-12), of either sign, of each
+  // term at most, beside the output's own rounding
+  __device__ __forceinline__ void add(const TileLane<HD>& at, const char* tile, int t, const f32x16& w) {
+#pragma unroll
+    for (int b = 0; b < 2; ++b) {
+      const int r = 8 * b;
+      const uint4 p = make_uint4(pack2<T>(w[r], w[r + 1]), pack2<T>(w[r + 2], w[r + 3]), pack2<T>(w[r + 4], w[r + 5]),
+                                 pack2<T>(w[r + 6], w[r + 7]));
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) sum[i] = mma32<T>(at.cols(tile, 2 * t + b, i), p, sum[i]);
+    }
+  }
+  // The same with only the rows from `first` to `last` of the tile.
+  __device__ __forceinline__ void add_only(const char* tile, int t, const f32x16& w, int first, int last) {
+    add_apart<HD, T>(sum, w, tile, 32 * t, [&](int k) { return first <= k && k <= last; });
+  }
+};
+
+// ------------------------------------------------------------------ queries
+template <int HD, CacheType T, int NW>
+__global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(PromptBwdArgs b, float2* stats) {
+  extern __shared__ __align__(16) char lds[];
+  constexpr int M = 32 * NW, KS = HD / 16;
+  const PromptArgs& a = b.fwd;
+  const int head = blockIdx.x % a.n_heads, item = blockIdx.x / a.n_heads;
+  SeqTile st;
+  if (!find_tile<M>(a.row_start, a.n_seq, a.rows, item, st)) return;
+  const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int kvh = head / (a.n_heads / a.n_kv_heads);
+  const SeqRows k = {a.k.p + st.row0 * a.k.ld + kvh * HD, a.k.ld}, v = {a.v.p + st.row0 * a.v.ld + kvh * HD, a.v.ld};
+  const int q0 = M * st.tile + 32 * wave, qi = q0 + (lane & 31);
+  const bool mine = qi < st.len;
+  const int64_t row = st.row0 + (int64_t)min(qi, st.len - 1);
+  const ScoreScale sc(a.scale);
+  uint4 q[KS], go[KS];
+  float d = 0.f;
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    const int f = head * HD + 16 * i + 8 * h;
+    q[i] = sc.turned(*reinterpret_cast<const uint4*>(a.q.p + row * a.q.ld + f));
+    go[i] = *reinterpret_cast<const uint4*>(b.dout.p + row * b.dout.ld + f);
+    const uint4 o = *reinterpret_cast<const uint4*>(a.o.p + row * a.o.ld + f);
+    const uint32_t x[4] = {go[i].x, go[i].y, go[i].z, go[i].w}, y[4] = {o.x, o.y, o.z, o.w};
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const float2 u = unpack2<T>(x[e]), w = unpack2<T>(y[e]);
+      d = fmaf(u.x, w.x, fmaf(u.y, w.y, d));
+    }
+  }
+  d = half_sum(d);
+  const float lse = lse_base2(a.lse[row * a.n_heads + head]);
+  if (mine && lane < 32) stats[(int64_t)head * a.rows + row] = make_float2(lse, d);
+  Column<HD, T> dq;
+  dq.begin();
+  const TileLane<HD> at;
+  const int last = (min(M * (st.tile + 1), st.len) - 1) / kTile, own = q0 < st.len ? q0 / kTile : -1;
+  auto tile = [&](int j, int which) { return lds + (2 * (j & 1) + which) * kTileBytes<HD>; };
+  // dS of the 32 keys from 32 t on of tile j, before the scale
+  auto ds_of = [&](int j, int t, bool masked) {
+    f32x16 s = zeros16(), dp;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) dp[r] = -d;
+#pragma unroll
+    for (int i = 0; i < KS; ++i) s = mma32<T>(at.rows(tile(j, 0), 32 * t, i), q[i], s);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) dp = mma32<T>(at.rows(tile(j, 1), 32 * t, i), go[i], dp);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.base2, -lse)) * dp[r];
+      if (masked && kTile * j + 32 * t + mma_row(r, h) > qi) s[r] = 0.f;
+    }
+    return s;
+  };
+  copy_tile<HD, NW>(tile(last, 0), k, kTile * last, st.len, wave);
+  copy_tile<HD, NW>(tile(last, 1), v, kTile * last, st.len, wave);
+  WAIT_VMCNT(0);
+  __syncthreads();
+  for (int j = last; j >= 0; --j) {
+    if (j > 0) {
+      copy_tile<HD, NW>(tile(j - 1, 0), k, kTile * (j - 1), st.len, wave);
+      copy_tile<HD, NW>(tile(j - 1, 1), v, kTile * (j - 1), st.len, wave);
+    }
+    if (j < own) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x16 s = ds_of(j, t, false);
+        dq.fit(s);
+        dq.add(at, tile(j, 0), t, s);
+      }
+    } else if (j == own) {
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        f32x16 s = ds_of(j, t, true);
+        dq.fit(s);
+        dq.add(at, tile(j, 0), t, s);
+      }
+      if (__builtin_expect(any_nan(dq.sum), 0)) {  // a masked key may have spoiled the sums: once more without it
+        dq.begin();
+#pragma nounroll
+        for (int t = 0; t < 2; ++t) {
+          f32x16 s = ds_of(j, t, true);
+          dq.fit(s);
+          dq.add_only(tile(j, 0), t, s, 0, qi - kTile * j);
+        }
+      }
+    }
+    WAIT_VMCNT(0);
+    __syncthreads();
+  }
+  if (own >= 0) store_row<HD, T>(b.dq.p + row * b.dq.ld + head * HD, dq.sum, a.scale / dq.unit, mine);
+}
+
+// ------------------------------------------------------------------ keys
+template <int HD, CacheType T, int NW>
+__global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats) {
+  extern __shared__ __align__(16) char lds[];
+  constexpr int M = 32 * NW, KS = HD / 16;
+  const PromptArgs& a = b.fwd;
+  const int kvh = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads, group = a.n_heads / a.n_kv_heads;
+  SeqTile st;
+  if (!find_tile<M>(a.row_start, a.n_seq, a.rows, item, st)) return;
+  const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int k0 = M * st.tile + 32 * wave, kj = k0 + (lane & 31);
+  const bool mine = kj < st.len;
+  const int64_t row = st.row0 + (int64_t)min(kj, st.len - 1);
+  const ScoreScale sc(a.scale);
+  uint4 k[KS], v[KS];
+#pragma unroll
+  for (int i = 0; i < KS; ++i) {
+    k[i] = sc.turned(*reinterpret_cast<const uint4*>(a.k.p + row * a.k.ld + kvh * HD + 16 * i + 8 * h));
+    v[i] = *reinterpret_cast<const uint4*>(a.v.p + row * a.v.ld + kvh * HD + 16 * i + 8 * h);
+  }
+  Column<HD, T> dk, dv;
+  const TileLane<HD> at;
+  const int first = M * st.tile / kTile, end = (st.len + kTile - 1) / kTile;        // tiles of queries
+  const int last_own = (min(M * (st.tile + 1), st.len) - 1) / kTile;                // of the workgroup's last key
+  const int own = k0 < st.len ? k0 / kTile : end;                                   // of this wave's keys: the one with masked pairs
+  auto tile = [&](int n, int which) { return lds + (2 * (n & 1) + which) * kTileBytes<HD>; };
+  auto stat = [&](int n) { return reinterpret_cast<float2*>(lds + 4 * kTileBytes<HD>) + (n & 1) * kTile; };
+  // tile j of head `head` into buffer n; waits for nothing
+  auto copy = [&](int n, int head, int j) {
+    const SeqRows q = {a.q.p + st.row0 * a.q.ld + head * HD, a.q.ld};
+    const SeqRows go = {b.dout.p + st.row0 * b.dout.ld + head * HD, b.dout.ld};
+    copy_tile<HD, NW>(tile(n, 0), q, kTile * j, st.len, wave);
+    copy_tile<HD, NW>(tile(n, 1), go, kTile * j, st.len, wave);
+    if (wave == 0) {  // rows behind the last have weights of 0
+      const int i = kTile * j + lane;
+      stat(n)[lane] = i < st.len ? stats[(int64_t)head * a.rows + st.row0 + i] : make_float2(INFINITY, 0.f);
+    }
+  };
+  // p = weights (times 2^15 in half precision) and ds of the 32 queries from 32 t on of tile j in buffer n
+  auto weights = [&](int n, int j, int t, bool masked, f32x16& p, f32x16& ds) {
+    p = zeros16();
+    float lse[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      const float2 x = stat(n)[32 * t + mma_row(r, h)];
+      lse[r] = x.x - kWeightExp<T>;
+      ds[r] = -x.y;
+    }
+#pragma unroll
+    for (int i = 0; i < KS; ++i) p = mma32<T>(at.rows(tile(n, 0), 32 * t, i), k[i], p);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) ds = mma32<T>(at.rows(tile(n, 1), 32 * t, i), v[i], ds);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], sc.base2, -lse[r]));
+      ds[r] *= p[r];
+      if (masked && kTile * j + 32 * t + mma_row(r, h) < kj) p[r] = ds[r] = 0.f;
+    }
+  };
+  // All heads' tiles j0 .. j1 - 1 in turn.
+  auto over = [&](int j0, int j1, auto&& take) {
+    if (j0 >= j1) return;
+    const int n = group * (j1 - j0);
+    int head = kvh * group, j = j0;
+    __syncthreads();  // what the buffers held has been used
+    copy(0, head, j);
+    WAIT_VMCNT(0);
+    __syncthreads();
+    for (int i = 0; i < n; ++i) {
+      const int now = j;
+      if (++j == j1) {
+        j = j0;
+        ++head;
+      }
+      if (i + 1 < n) copy(i + 1, head, j);
+      take(i, now);
+      WAIT_VMCNT(0);
+      __syncthreads();
+    }
+  };
+  // First the tiles part of whose pairs are masked, of all heads; then the whole ones.
+  dk.begin();
+  dv.begin();
+  over(first, last_own + 1, [&](int n, int j) {
+    if (j != own) return;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 p, ds;
+      weights(n, j, t, true, p, ds);
+      dv.add(at, tile(n, 1), t, p);
+      dk.fit(ds);
+      dk.add(at, tile(n, 0), t, ds);
+    }
+  });
+  const bool spoiled = any_nan(dk.sum) || any_nan(dv.sum);
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(__syncthreads_or(spoiled)), 0)) {  // masked queries may have spoiled the sums: once more without them
+    if (spoiled) {
+      dk.begin();
+      dv.begin();
+    }
+    over(first, last_own + 1, [&](int n, int j) {
+      if (j != own || !spoiled) return;
+#pragma nounroll
+      for (int t = 0; t < 2; ++t) {
+        f32x16 p, ds;
+        weights(n, j, t, true, p, ds);
+        dv.add_only(tile(n, 1), t, p, kj - kTile * j, kTile);
+        dk.fit(ds);
+        dk.add_only(tile(n, 0), t, ds, kj - kTile * j, kTile);
+      }
+    });
+  }
+  over(first + 1, end, [&](int n, int j) {
+    if (j <= own) return;
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 p, ds;
+      weights(n, j, t, false, p, ds);
+      dv.add(at, tile(n, 1), t, p);
+      dk.fit(ds);
+      dk.add(at, tile(n, 0), t, ds);
+    }
+  });
+  if (own == end) return;
+  constexpr float kUnit = T == kBf16 ? 1.f : 0x1p-15f;
+  store_row<HD, T>(b.dk.p + row * b.dk.ld + kvh * HD, dk.sum, a.scale * kUnit / dk.unit, mine);
+  store_row<HD, T>(b.dv.p + row * b.dv.ld + kvh * HD, dv.sum, kUnit, mine);
+}
+
+template <int HD, CacheType T>
+hipError_t launch(const PromptBwdArgs& b, hipStream_t s) {
+  constexpr int NW = 4, kDq = 4 * kTileBytes<HD>, kDkv = kDq + 2 * kTile * (int)sizeof(float2);
+  static LdsLimit dq_limit, dkv_limit;
+  const auto dq = prompt_dq_kernel<HD, T, NW>;
+  const auto dkv = prompt_dkv_kernel<HD, T, NW>;
+  hipError_t e = dq_limit.allow((const void*)dq, kDq);
+  if (e == hipSuccess) e = dkv_limit.allow((const void*)dkv, kDkv);
+  if (e != hipSuccess) return e;
+  const long long items = seq_items(b.fwd.rows, b.fwd.n_seq, 32 * NW);
+  float2* stats = static_cast<float2*>(b.ws);
+  hipLaunchKernelGGL(dq, dim3((unsigned)(items * b.fwd.n_heads)), dim3(64 * NW), kDq, s, b, stats);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(dkv, dim3((unsigned)(items * b.fwd.n_kv_heads)), dim3(64 * NW), kDkv, s, b, stats);
+  return hipGetLastError();
+}
+
+template <CacheType T>
+hipError_t launch_type(const PromptBwdArgs& b, hipStream_t s) {
+  if (b.fwd.head_dim == 64) return launch<64, T>(b, s);
+  if (b.fwd.head_dim == 128) return launch<128, T>(b, s);
+  if (b.fwd.head_dim == 256) return launch<256, T>(b, s);
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+size_t prompt_bwd_bytes(int rows, int n_seq, int n_heads, int n_kv_heads, int head_dim) {
+  return ((size_t)rows * n_heads * sizeof(float2) + 255) / 256 * 256;
+}
+
+hipError_t launch_prompt_attn_bwd(const PromptBwdArgs& b, hipStream_t s) {
+  return b.fwd.type == kBf16 ? launch_type<kBf16>(b, s) : launch_type<kF16>(b, s);
+}
+
+}  // namespace vla

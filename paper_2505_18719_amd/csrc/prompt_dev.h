@@ -1,0 +1,223 @@
+// Device code that attention over whole prompts and its gradient share: tiles of rows in LDS, 32x32x16 MFMA operands from them,
+// and the way from a workgroup to its sequence.
+//
+// Every product has the softmax's own index on the MFMA's columns: a wave holds 32 queries (or keys) as columns, lane % 32, and
+// the other index on the rows, of which lane half h = lane / 32 has rows 8 i + 4 h + e, i, e = 0 .. 3, in registers 4 i + e.  Eight
+// of these (i = 2 b, 2 b + 1) are the B operand of step b of the next product, if its A operand's k are taken in the same order:
+// two transposed reads of 4 rows each, 4 h .. and 8 + 4 h .. of the step's 16.  So weights never leave their registers.
+#pragma once
+
+#include "cache.h"
+#include "common.h"
+
+namespace vla {
+
+constexpr int kTile = 64;  // rows of a tile in LDS
+constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
+
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+
+template <CacheType T>
+__device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, const f32x16& c) {
+  if constexpr (T == kBf16) return mfma32(as_bf16x8(a), as_bf16x8(b), c);
+  else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// Two numbers of the type, to nearest even.
+template <CacheType T>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  if constexpr (T == kBf16) return pack2bf(lo, hi);
+  else return __builtin_bit_cast(uint32_t, (f16x2){(_Float16)lo, (_Float16)hi});
+}
+template <CacheType T>
+__device__ __forceinline__ float2 unpack2(uint32_t v) {
+  if constexpr (T == kBf16) return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
+  const f16x2 h = __builtin_bit_cast(f16x2, v);
+  return make_float2((float)h[0], (float)h[1]);
+}
+// The scale of the scores to base 2, positive: its sign goes into one of the factors, and a scale of 0 makes that factor 0, so that
+// the largest product has the largest score and a masked one's -inf stays -inf.
+struct ScoreScale {
+  float base2;
+  uint32_t sign, keep;
+  __device__ __forceinline__ explicit ScoreScale(float s)
+      : base2(s == 0.f ? 1.f : fabsf(s) * kLog2e), sign(s < 0.f ? 0x80008000u : 0u), keep(s == 0.f ? 0u : ~0u) {}
+  __device__ __forceinline__ uint4 turned(const uint4& x) const {
+    return make_uint4((x.x ^ sign) & keep, (x.y ^ sign) & keep, (x.z ^ sign) & keep, (x.w ^ sign) & keep);
+  }
+};
+// Half-precision weights are held 2^15 times as large: the largest stays below 65504, and one is rounded to fewer than 11 bits only
+// below 2^-29 of the largest.
+template <CacheType T>
+constexpr float kWeightExp = T == kBf16 ? 0.f : 15.f;
+__device__ __forceinline__ f32x16 zeros16() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.f;
+  return z;
+}
+
+// Max / sum over the two lanes that share lane % 32.
+__device__ __forceinline__ float half_max(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float v) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// MFMA row of register r in lane half h.
+__device__ __forceinline__ constexpr int mma_row(int r, int h) { return 8 * (r >> 2) + 4 * h + (r & 3); }
+
+// ------------------------------------------------------------------ tiles in LDS
+// Row R of a tile lies at R * 2 HD bytes, its 16-byte chunk j at place j ^ swz(R).  Both ways to read then spread over all
+// banks: the same chunk of 16 consecutive rows (128-bit reads), and 64 bytes of 4 consecutive rows (transposed reads).
+template <int HD>
+__device__ __forceinline__ int swz(int R) {
+  return HD == 64 ? ((R >> 1 & 1) << 2 | (R >> 2 & 3)) : ((R & 3) << 2 | (R >> 2 & 3));
+}
+template <int HD>
+constexpr int kTileBytes = kTile * HD * 2;
+
+// Lane addresses into a tile.
+template <int HD>
+struct TileLane {
+  uint32_t row;   // chunk 0 of row lane % 32, before its place is turned
+  uint32_t turn;  // 16 (lane / 32 ^ swz of that row)
+  uint32_t col;   // first transposed read of features 0 .. 31
+  __device__ __forceinline__ TileLane() {
+    const int lane = threadIdx.x & 63, h = lane >> 5, i = lane & 15;
+    row = (lane & 31) * HD * 2;
+    turn = 16 * (h ^ swz<HD>(lane & 31));
+    const int r = 4 * h + (i >> 2);
+    col = r * HD * 2 + 16 * ((2 * (lane >> 4 & 1) + (i >> 1 & 1)) ^ swz<HD>(r)) + 8 * (i & 1);
+  }
+  // Row lane % 32 of the 32 from r0 on (0 or 32), features 16 ks + 8 (lane / 32) .. + 8.
+  __device__ __forceinline__ uint4 rows(const char* tile, int r0, int ks) const {
+    return *reinterpret_cast<const uint4*>(tile + r0 * HD * 2 + row + (turn ^ 32 * ks));
+  }
+  // Features 32 mb + lane % 32, rows 16 b + 4 (lane / 32) .. + 4 and 8 more on.
+  __device__ __forceinline__ uint4 cols(const char* tile, int b, int mb) const {
+    // eight rows on, bit 1 of the place turns; 32 features on, bits 2 and up
+    const char* p = tile + 16 * b * HD * 2;
+    return __builtin_bit_cast(uint4, lds_read_tr(p + (col ^ 64 * mb), p + 8 * HD * 2 + (col ^ 32 ^ 64 * mb)));
+  }
+};
+
+// The rows of one head of a sequence, from its first on.
+struct SeqRows {
+  const bf16_t* p;
+  int64_t ld;
+};
+// Copies rows r0 .. r0 + 63 of a sequence of `len` rows into a tile (rows behind its last: that one), 1 KB per wave and
+// instruction; the waves of the workgroup share them.
+template <int HD, int NW>
+__device__ __forceinline__ void copy_tile(char* tile, const SeqRows& x, int r0, int len, int wave) {
+  constexpr int CH = HD / 8, RPK = 64 / CH, N = kTile / RPK;  // chunks of a row, rows of a copy, copies
+  const int lane = threadIdx.x & 63;
+  const uint32_t lb = (uint32_t)(uintptr_t)((lds_ptr_t*)tile);
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc((void*)(x.p + (int64_t)r0 * x.ld), (short)0, 0x7fffffff, 0x00020000);
+#pragma unroll
+  for (int i = 0; i < (N + NW - 1) / NW; ++i) {
+    const int j = i * NW + wave;
+    if (N % NW != 0 && j >= N) break;
+    const int R = j * RPK + lane / CH;
+    lds_dma16(lb + j * 1024, (uint32_t)(min(R, len - 1 - r0) * (int)x.ld + 8 * ((lane % CH) ^ swz<HD>(R))) * 2, rs, 0);
+  }
+}
+
+// acc[mb][r] += sum over the 32 rows k of a tile from r0 on of w[k] x[k][feature], features 32 mb + mma_row(r): one product on the
+// vector units, with every term for which keep(k) is false left out whatever x[k] is.  w: the weights of this lane's column, as
+// the two halves hold them.  Only where infinite or NaN elements lie in a tile part of whose pairs are masked.
+template <int HD, CacheType T, class F>
+__device__ __forceinline__ void add_apart(f32x16 (&acc)[HD / 32], f32x16 w, const char* tile, int r0, F keep) {
+  const int lane = threadIdx.x & 63, h = lane >> 5;
+#pragma nounroll
+  for (int n = 0; n < 32; ++n) {  // row n's weight is in half n / 4 % 2, register 4 (n / 8) + n % 4
+    float p = w[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) p = 4 * (n >> 3) + (n & 3) == r ? w[r] : p;
+    p = __shfl(p, (lane & 31) + 32 * (n >> 2 & 1), kWave);
+    const int k = r0 + n;
+    const bool use = keep(k);
+#pragma unroll
+    for (int mb = 0; mb < HD / 32; ++mb)
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        const uint2 x = *reinterpret_cast<const uint2*>(tile + k * HD * 2 + 16 * ((4 * mb + c) ^ swz<HD>(k)) + 8 * h);
+        const float2 lo = unpack2<T>(x.x), hi = unpack2<T>(x.y);
+        const float v[4] = {lo.x, lo.y, hi.x, hi.y};
+#pragma unroll
+        for (int f = 0; f < 4; ++f) acc[mb][4 * c + f] = use ? fmaf(p, v[f], acc[mb][4 * c + f]) : acc[mb][4 * c + f];
+      }
+  }
+}
+
+// Whether an element of acc is NaN, in any lane.
+template <int N>
+__device__ __forceinline__ bool any_nan(const f32x16 (&acc)[N]) {
+  float s[4] = {0.f, 0.f, 0.f, 0.f};  // NaN where a term is
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r & 3] += acc[i][r];
+  return __any(__builtin_isnan((s[0] + s[1]) + (s[2] + s[3])));
+}
+
+// Writes this lane's column of acc, times `mul`, as a row of HD numbers of the type: 16 bytes per store, the two halves of the wave
+// in turn.
+template <int HD, CacheType T>
+__device__ __forceinline__ void store_row(bf16_t* row, const f32x16 (&acc)[HD / 32], float mul, bool write) {
+  const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int mb = 0; mb < HD / 32; ++mb)
+#pragma unroll
+    for (int i = 0; i < 4; i += 2) {
+      uint32_t a[2], b[2];  // features 8 i + 4 h .. + 4, and eight on
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        a[e] = pack2<T>(acc[mb][4 * i + 2 * e] * mul, acc[mb][4 * i + 2 * e + 1] * mul);
+        b[e] = pack2<T>(acc[mb][4 * i + 4 + 2 * e] * mul, acc[mb][4 * i + 5 + 2 * e] * mul);
+      }
+      // lane half 0 gets features 8 i .. + 8, half 1 those eight on
+      const auto x = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
+      const auto y = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+      if (write) *reinterpret_cast<uint4*>(row + 32 * mb + 8 * i + 8 * h) = make_uint4(x[0], y[0], x[1], y[1]);
+    }
+}
+
+// ------------------------------------------------------------------ from a workgroup to its rows
+// Sequence s has items row_start[s] / M + s and on, one per M of its rows begun: enough of them, and none of the next sequence's,
+// whatever the lengths, so that a workgroup finds its sequence by a search of row_start; the items in between are empty.
+struct SeqTile {
+  int row0, len, tile;  // first row and rows of the sequence, the item's M rows
+};
+inline __host__ __device__ long long seq_items(int rows, int n_seq, int M) { return (long long)rows / M + n_seq; }
+
+template <int M>
+__device__ __forceinline__ bool find_tile(const int32_t* row_start, int n_seq, int rows, int item, SeqTile& t) {
+  const int lane = threadIdx.x & 63;
+  int lo = 0, n = n_seq;
+  for (;;) {
+    const int step = (n + kWave - 1) / kWave, at = lo + lane * step;
+    const bool before = (long long)lane * step < n && min(max(row_start[min(at, n_seq)], 0), rows) / M + at <= item;
+    const int found = __popcll(__ballot(before));
+    if (found == 0) return false;
+    lo += (found - 1) * step;
+    n = min(step, n - (found - 1) * step);
+    if (step == 1) break;
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  t.row0 = __builtin_amdgcn_readfirstlane(row_start[lo]);
+  const int end = __builtin_amdgcn_readfirstlane(row_start[lo + 1]);
+  if (t.row0 < 0 || end <= t.row0 || end > rows) return false;
+  t.len = end - t.row0;
+  const int tiles = (t.len + M - 1) / M, nth = item - (t.row0 / M + lo);
+  if (nth >= tiles) return false;
+  t.tile = tiles - 1 - nth;  // the longest rows of a sequence first
+  return true;
+}
+
+}  // namespace vla

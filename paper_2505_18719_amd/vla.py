@@ -2,8 +2,8 @@
 
 Every step of the rollout path runs in the HIP library; this module only
 passes device pointers of torch tensors, the current HIP stream and host
-arrays through the C ABI of ``include/vla.h``, ``include/vla_learn.h`` and
-``include/vla_cache.h``.  Importing it fails loudly if
+arrays through the C ABI of ``include/vla.h``, ``include/vla_learn.h``,
+``include/vla_cache.h`` and ``include/vla_prompt.h``.  Importing it fails loudly if
 the library has not been built.
 """
 from __future__ import annotations
@@ -28,7 +28,8 @@ EXPORTS = ("vla_workspace_size", "vla_create", "vla_prefill", "vla_decode_action
            "vla_last_error", "vla_extract_actions", "vla_gae", "vla_ppo_clip", "vla_logprob_backward",
            "vla_train_workspace_size", "vla_ppo_lora_grads", "vla_kv_plan", "vla_rope_freqs", "vla_qk_norm_rope",
            "vla_qk_norm_rope_workspace_size", "vla_qk_norm_rope_backward", "vla_paged_attention_workspace_size",
-           "vla_paged_attention")
+           "vla_paged_attention", "vla_prompt_attention", "vla_prompt_attention_backward_workspace_size",
+           "vla_prompt_attention_backward")
 # projections a LoRA adapter merges into (VLA_PROJ_* order), by weight-dict key
 PROJECTIONS = ("wq", "wk", "wv", "wo", "wgate", "wup", "wdown")
 PROF_CATEGORIES = ("prefill_gemm", "prefill_attn", "decode_gemm", "decode_attn", "decode_layer")
@@ -105,6 +106,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vla_paged_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(size)]
     lib.vla_paged_attention.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp, f32, vp, i64, vp,
                                         vp, size, vp]
+    lib.vla_prompt_attention.argtypes = [i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, f32, vp, i64, vp, vp]
+    lib.vla_prompt_attention_backward_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(size)]
+    lib.vla_prompt_attention_backward.argtypes = [i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp,
+                                                  i64, vp, f32, vp, i64, vp, i64, vp, i64, vp, size, vp]
     lib.vla_profile_begin.argtypes = [vp, ctypes.c_uint32]
     lib.vla_profile_end.argtypes = [vp, vp, vp, vp]
     lib.vla_destroy.argtypes = [vp]
@@ -722,3 +727,67 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
             _at(lens, torch.int32, index, "lens", n), scale, op, os_, _at(lse, torch.float32, index, "lse", n, H),
             _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
     return out
+
+
+# ---------------------------------------------------------------- attention over whole prompts (vla_prompt.h)
+def _sequences(row_start: torch.Tensor, index: int):
+    """(address, sequences) of an int32 row_start [n_seq + 1] on device `index`."""
+    n = row_start.shape[0] if row_start.dim() == 1 else 0
+    if n < 1:
+        raise ValueError("row_start must be [n_seq + 1]")
+    return _at(row_start, torch.int32, index, "row_start", n), n - 1
+
+
+def prompt_attention(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, row_start: torch.Tensor, scale: float,
+                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Causal attention [rows, n_heads, head_dim] of the packed sequences row_start[s] .. row_start[s + 1] - 1 of q [rows,
+    n_heads, head_dim], k and v [rows, n_kv_heads, head_dim] (vla_prompt_attention); lse fp32 [rows, n_heads], if passed in,
+    receives the log-sum-exp of the scores.  Rows of no sequence are left as they were (of an output allocated here:
+    undefined).  Takes no part in autograd: its gradient is prompt_attention_backward."""
+    lib = _lib or load_library()
+    rows, H, hd, dt, index = _heads(q, "q")
+    dtype, K = q.dtype, k.shape[1]
+    out, op, os_ = _out_rows(out, q, index, "out", rows, H, hd)
+    qp, qs = _head_rows(q, dtype, index, "q", rows, H, hd)
+    kp, ks = _head_rows(k, dtype, index, "k", rows, K, hd)
+    vp, vs = _head_rows(v, dtype, index, "v", rows, K, hd)
+    start, n = _sequences(row_start, index)
+    _launch(index, lib.vla_prompt_attention, rows, n, H, K, hd, dt, qp, qs, kp, ks, vp, vs, start, scale, op, os_,
+            _at(lse, torch.float32, index, "lse", rows, H))
+    return out
+
+
+def prompt_attention_backward_workspace(q: torch.Tensor, k: torch.Tensor, row_start: torch.Tensor) -> torch.Tensor:
+    """The workspace of prompt_attention_backward for calls of these shapes."""
+    lib = load_library()
+    n = ctypes.c_size_t()
+    _check(lib.vla_prompt_attention_backward_workspace_size(q.shape[0], row_start.shape[0] - 1, q.shape[1], k.shape[1],
+                                                            q.shape[2], ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=q.device)
+
+
+def prompt_attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tensor, lse: torch.Tensor,
+                              dout: torch.Tensor, row_start: torch.Tensor, scale: float,
+                              dq: Optional[torch.Tensor] = None, dk: Optional[torch.Tensor] = None,
+                              dv: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None):
+    """(dq, dk, dv) of prompt_attention from its inputs, its outputs out and lse, and the gradient dout of out
+    (vla_prompt_attention_backward).  Rows of no sequence are left as they were (of a gradient allocated here: zeros)."""
+    lib = _lib or load_library()
+    rows, H, hd, dt, index = _heads(q, "q")
+    dtype, K = q.dtype, k.shape[1]
+    dq = torch.zeros((rows, H, hd), dtype=dtype, device=q.device) if dq is None else dq
+    dk = torch.zeros((rows, K, hd), dtype=dtype, device=q.device) if dk is None else dk
+    dv = torch.zeros((rows, K, hd), dtype=dtype, device=q.device) if dv is None else dv
+    places = []
+    for t, name, heads in ((q, "q", H), (k, "k", K), (v, "v", K), (out, "out", H), (dout, "dout", H), (dq, "dq", H),
+                           (dk, "dk", K), (dv, "dv", K)):
+        places.append(_head_rows(t, dtype, index, name, rows, heads, hd))
+    q_, k_, v_, o_, do_, dq_, dk_, dv_ = places
+    start, n = _sequences(row_start, index)
+    if workspace is None:
+        workspace = prompt_attention_backward_workspace(q, k, row_start)
+    n_ws = workspace.shape[0]
+    _launch(index, lib.vla_prompt_attention_backward, rows, n, H, K, hd, dt, *q_, *k_, *v_, *o_,
+            _at(lse, torch.float32, index, "lse", rows, H), *do_, start, scale, *dq_, *dk_, *dv_,
+            _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
+    return dq, dk, dv
