@@ -193,6 +193,42 @@ int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int3
                         float scale, void* out, int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes,
                         void* stream);
 
+/* ---- the cache in 8-bit numbers ----
+ * Half the bytes of the pages above: the same pages with elements of one byte
+ * (sign, 4 bits of exponent, 3 of mantissa; largest 448, no infinities, 0x7f
+ * and 0xff NaN), and a scale per token and head,
+ *     k_pages   [n_pages, n_kv_heads, 16, head_dim]    k_scales  fp32 [n_pages, n_kv_heads, 16]
+ *     v_pages   [n_pages, n_kv_heads, head_dim, 16]    v_scales  the same
+ * each element standing for its number times its token's scale.  Pages start
+ * on 16 bytes, scales on 4.
+ *
+ * vla_kv_append_f8 writes row r of k and v [rows, n_kv_heads, head_dim] to
+ * slot row_slot[r]: with t the largest size of an element of the head (at
+ * least 2^-100), the scale t / 448 and each element x as x 448 / t rounded to
+ * nearest even: off by at most 2^-4 of itself or 2^-10 t / 448.  A head with
+ * an infinite or NaN element is stored as NaN with a NaN scale.
+ * vla_kv_read_f8 is its reverse: rows k and v of `dtype` from the slots, each
+ * product rounded once (in fp16 past 65504 to infinity).
+ * In both a row whose slot lies outside [0, 16 n_pages) is passed over:
+ * neither the cache nor its rows are written.  Slots of an append are
+ * distinct.  rows == 0 is a no-op; rows n_kv_heads head_dim / 8 below 2^32. */
+int vla_kv_append_f8(int32_t rows, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void* k, int64_t ld_k,
+                     const void* v, int64_t ld_v, void* k_pages, void* v_pages, float* k_scales, float* v_scales,
+                     int32_t n_pages, const int32_t* row_slot, void* stream);
+int vla_kv_read_f8(int32_t rows, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void* k_pages,
+                   const void* v_pages, const float* k_scales, const float* v_scales, int32_t n_pages,
+                   const int32_t* row_slot, void* k, int64_t ld_k, void* v, int64_t ld_v, void* stream);
+
+/* vla_paged_attention over such a cache, with its arguments, its workspace
+ * (vla_paged_attention_workspace_size) and its results for the elements' values;
+ * a NaN among the keys of a length gives its heads NaN, among the values its
+ * features'. */
+int vla_paged_attention_f8(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                           const void* q, int64_t ld_q, const void* k_pages, const void* v_pages,
+                           const float* k_scales, const float* v_scales, int32_t n_pages, const int32_t* page_table,
+                           int64_t ld_table, int32_t max_pages, const int32_t* lens, float scale, void* out,
+                           int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

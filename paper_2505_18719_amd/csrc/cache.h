@@ -5,8 +5,9 @@
 
 namespace vla {
 
-// Types of q, k, v, pages and outputs (VLA_DTYPE_*).
-enum CacheType { kBf16 = 0, kF16 = 1 };
+// Types of q, k, v, pages and outputs (VLA_DTYPE_*); F8: with pages of 8-bit numbers (4 bits of exponent, 3 of mantissa), in
+// device code only.
+enum CacheType { kBf16 = 0, kF16 = 1, kBf16F8 = 2, kF16F8 = 3 };
 
 // Pages, rows and slots of a step's new tokens (vla_kv_plan).
 struct KvPlanArgs {
@@ -91,8 +92,28 @@ struct PagedAttnArgs {
   int64_t ld_o;
   float* lse;                  // [n_env, n_heads], or null
   void* ws;                    // paged_attn_bytes(...) bytes
+  const float* k_scales;       // 8-bit pages: [n_pages, n_kv_heads, kPage], else unused
+  const float* v_scales;
 };
 size_t paged_attn_bytes(int n_env, int n_heads, int n_kv_heads, int head_dim, int max_pages);
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
+hipError_t launch_paged_attn_f8(const PagedAttnArgs& a, hipStream_t s);  // pages of 8-bit numbers
+
+// Keys and values into pages of 8-bit numbers, and back (vla_kv_append_f8, vla_kv_read_f8).
+struct KvF8Args {
+  int rows, n_kv_heads, head_dim;
+  CacheType type;
+  HeadRows k, v;               // in, or out when read
+  uint8_t* k_pages;            // [n_pages, n_kv_heads, kPage, head_dim]
+  uint8_t* v_pages;            // [n_pages, n_kv_heads, head_dim, kPage]
+  float* k_scales;             // [n_pages, n_kv_heads, kPage]
+  float* v_scales;
+  int n_pages;
+  const int32_t* row_slot;     // [rows]
+};
+// Whether one launch takes that many rows.
+bool kv_f8_fits(int rows, int n_kv_heads, int head_dim);
+hipError_t launch_kv_append_f8(const KvF8Args& a, hipStream_t s);
+hipError_t launch_kv_read_f8(const KvF8Args& a, hipStream_t s);
 
 }  // namespace vla

@@ -185,31 +185,92 @@ int vla_paged_attention_workspace_size(int32_t n_env, int32_t n_heads, int32_t n
   return set_error(VLA_OK, "");
 }
 
+// What the attentions over pages of either kind check alike.
+static int check_paged(const PagedAttnArgs& a, int64_t workspace_bytes) {
+  int rc = check_attention(a.n_env, a.n_heads, a.n_kv_heads, a.head_dim, a.max_pages);
+  if (rc == VLA_OK) rc = check_heads(a.n_heads, a.n_kv_heads, a.head_dim, a.type);
+  if (rc != VLA_OK) return rc;
+  if (a.n_pages < 0) return set_error(VLA_EINVAL, "negative size");
+  if (a.n_pages >= 1 << 27) return set_error(VLA_EUNSUPPORTED, "n_pages must be below 2^27");
+  if ((rc = check_scale(a.scale)) != VLA_OK || a.n_env == 0) return rc;
+  const int64_t width = (int64_t)a.n_heads * a.head_dim;
+  if ((rc = check_rows("q", a.q, a.ld_q, width)) || (rc = check_rows("out", a.o, a.ld_o, width))) return rc;
+  if (a.ld_table < a.max_pages || a.ld_table > (int64_t)1 << 40) return set_error(VLA_EINVAL, "ld_table must hold a row of the page table");
+  if (!a.lens || (a.max_pages > 0 && !a.page_table) || (a.n_pages > 0 && (!a.pages.k || !a.pages.v)))
+    return set_error(VLA_EINVAL, "NULL argument");
+  if (!aligned(a.pages.k) || !aligned(a.pages.v)) return set_error(VLA_EINVAL, "pages must start on 16 bytes");
+  const size_t need = paged_attn_bytes(a.n_env, a.n_heads, a.n_kv_heads, a.head_dim, a.max_pages);
+  if (need > 0 && (!a.ws || !aligned(a.ws, 256) || (size_t)workspace_bytes < need))
+    return set_error(VLA_EWORKSPACE, "workspace smaller than vla_paged_attention_workspace_size() or misaligned");
+  return VLA_OK;
+}
+
 int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
                         const void* q, int64_t ld_q, const void* k_pages, const void* v_pages, int32_t n_pages,
                         const int32_t* page_table, int64_t ld_table, int32_t max_pages, const int32_t* lens,
                         float scale, void* out, int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes,
                         void* stream) {
-  int rc = check_attention(n_env, n_heads, n_kv_heads, head_dim, max_pages);
-  if (rc == VLA_OK) rc = check_heads(n_heads, n_kv_heads, head_dim, dtype);
-  if (rc != VLA_OK) return rc;
-  if (n_pages < 0) return set_error(VLA_EINVAL, "negative size");
-  if (n_pages >= 1 << 27) return set_error(VLA_EUNSUPPORTED, "n_pages must be below 2^27");
-  if ((rc = check_scale(scale)) != VLA_OK) return rc;
-  if (n_env == 0) return set_error(VLA_OK, "");
-  const int64_t width = (int64_t)n_heads * head_dim;
-  if ((rc = check_rows("q", q, ld_q, width)) || (rc = check_rows("out", out, ld_o, width))) return rc;
-  if (ld_table < max_pages || ld_table > (int64_t)1 << 40) return set_error(VLA_EINVAL, "ld_table must hold a row of the page table");
-  if (!lens || (max_pages > 0 && !page_table) || (n_pages > 0 && (!k_pages || !v_pages)))
-    return set_error(VLA_EINVAL, "NULL argument");
-  if (!aligned(k_pages) || !aligned(v_pages)) return set_error(VLA_EINVAL, "pages must start on 16 bytes");
-  const size_t need = paged_attn_bytes(n_env, n_heads, n_kv_heads, head_dim, max_pages);
-  if (need > 0 && (!workspace || !aligned(workspace, 256) || workspace_bytes < need))
-    return set_error(VLA_EWORKSPACE, "workspace smaller than vla_paged_attention_workspace_size() or misaligned");
   PagedAttnArgs a{n_env, n_heads, n_kv_heads, head_dim, static_cast<CacheType>(dtype), static_cast<const bf16_t*>(q),
                   ld_q, {static_cast<bf16_t*>(const_cast<void*>(k_pages)), static_cast<bf16_t*>(const_cast<void*>(v_pages))},
-                  n_pages, page_table, ld_table, max_pages, lens, scale, static_cast<bf16_t*>(out), ld_o, lse, workspace};
+                  n_pages, page_table, ld_table, max_pages, lens, scale, static_cast<bf16_t*>(out), ld_o, lse, workspace,
+                  nullptr, nullptr};
+  const int rc = check_paged(a, workspace_bytes);
+  if (rc != VLA_OK) return rc;
+  if (n_env == 0) return set_error(VLA_OK, "");
   return hip_status("vla_paged_attention", launch_paged_attn(a, static_cast<hipStream_t>(stream)));
+}
+
+int vla_paged_attention_f8(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
+                           const void* q, int64_t ld_q, const void* k_pages, const void* v_pages,
+                           const float* k_scales, const float* v_scales, int32_t n_pages, const int32_t* page_table,
+                           int64_t ld_table, int32_t max_pages, const int32_t* lens, float scale, void* out,
+                           int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  PagedAttnArgs a{n_env, n_heads, n_kv_heads, head_dim, static_cast<CacheType>(dtype), static_cast<const bf16_t*>(q),
+                  ld_q, {static_cast<bf16_t*>(const_cast<void*>(k_pages)), static_cast<bf16_t*>(const_cast<void*>(v_pages))},
+                  n_pages, page_table, ld_table, max_pages, lens, scale, static_cast<bf16_t*>(out), ld_o, lse, workspace,
+                  k_scales, v_scales};
+  const int rc = check_paged(a, workspace_bytes);
+  if (rc != VLA_OK) return rc;
+  if (n_env == 0) return set_error(VLA_OK, "");
+  if (n_pages > 0 && (!k_scales || !v_scales)) return set_error(VLA_EINVAL, "NULL argument");
+  return hip_status("vla_paged_attention_f8", launch_paged_attn_f8(a, static_cast<hipStream_t>(stream)));
+}
+
+static int check_kv_f8(const KvF8Args& a) {
+  if (a.rows < 0 || a.n_pages < 0) return set_error(VLA_EINVAL, "negative size");
+  if (a.n_pages >= 1 << 27) return set_error(VLA_EUNSUPPORTED, "n_pages must be below 2^27");
+  int rc = check_heads(1, a.n_kv_heads, a.head_dim, a.type);
+  if (rc != VLA_OK || a.rows == 0) return rc;
+  if (!kv_f8_fits(a.rows, a.n_kv_heads, a.head_dim)) return set_error(VLA_EUNSUPPORTED, "too many rows for one call");
+  const int64_t width = (int64_t)a.n_kv_heads * a.head_dim;
+  if ((rc = check_rows("k", a.k.p, a.k.ld, width)) || (rc = check_rows("v", a.v.p, a.v.ld, width))) return rc;
+  if (!a.row_slot || (a.n_pages > 0 && (!a.k_pages || !a.v_pages || !a.k_scales || !a.v_scales)))
+    return set_error(VLA_EINVAL, "NULL argument");
+  if (!aligned(a.k_pages) || !aligned(a.v_pages)) return set_error(VLA_EINVAL, "pages must start on 16 bytes");
+  return VLA_OK;
+}
+
+int vla_kv_append_f8(int32_t rows, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void* k, int64_t ld_k,
+                     const void* v, int64_t ld_v, void* k_pages, void* v_pages, float* k_scales, float* v_scales,
+                     int32_t n_pages, const int32_t* row_slot, void* stream) {
+  const KvF8Args a{rows, n_kv_heads, head_dim, static_cast<CacheType>(dtype), rows_of(k, ld_k), rows_of(v, ld_v),
+                   static_cast<uint8_t*>(k_pages), static_cast<uint8_t*>(v_pages), k_scales, v_scales, n_pages, row_slot};
+  const int rc = check_kv_f8(a);
+  if (rc != VLA_OK) return rc;
+  if (rows == 0) return set_error(VLA_OK, "");
+  return hip_status("vla_kv_append_f8", launch_kv_append_f8(a, static_cast<hipStream_t>(stream)));
+}
+
+int vla_kv_read_f8(int32_t rows, int32_t n_kv_heads, int32_t head_dim, int32_t dtype, const void* k_pages,
+                   const void* v_pages, const float* k_scales, const float* v_scales, int32_t n_pages,
+                   const int32_t* row_slot, void* k, int64_t ld_k, void* v, int64_t ld_v, void* stream) {
+  const KvF8Args a{rows, n_kv_heads, head_dim, static_cast<CacheType>(dtype), rows_of(k, ld_k), rows_of(v, ld_v),
+                   static_cast<uint8_t*>(const_cast<void*>(k_pages)), static_cast<uint8_t*>(const_cast<void*>(v_pages)),
+                   const_cast<float*>(k_scales), const_cast<float*>(v_scales), n_pages, row_slot};
+  const int rc = check_kv_f8(a);
+  if (rc != VLA_OK) return rc;
+  if (rows == 0) return set_error(VLA_OK, "");
+  return hip_status("vla_kv_read_f8", launch_kv_read_f8(a, static_cast<hipStream_t>(stream)));
 }
 
 }  // extern "C"

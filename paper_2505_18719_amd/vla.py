@@ -28,7 +28,7 @@ EXPORTS = ("vla_workspace_size", "vla_create", "vla_prefill", "vla_decode_action
            "vla_last_error", "vla_extract_actions", "vla_gae", "vla_ppo_clip", "vla_logprob_backward",
            "vla_train_workspace_size", "vla_ppo_lora_grads", "vla_kv_plan", "vla_rope_freqs", "vla_qk_norm_rope",
            "vla_qk_norm_rope_workspace_size", "vla_qk_norm_rope_backward", "vla_paged_attention_workspace_size",
-           "vla_paged_attention", "vla_prompt_attention", "vla_prompt_attention_backward_workspace_size",
+           "vla_paged_attention", "vla_kv_append_f8", "vla_kv_read_f8", "vla_paged_attention_f8", "vla_prompt_attention", "vla_prompt_attention_backward_workspace_size",
            "vla_prompt_attention_backward")
 # projections a LoRA adapter merges into (VLA_PROJ_* order), by weight-dict key
 PROJECTIONS = ("wq", "wk", "wv", "wo", "wgate", "wup", "wdown")
@@ -106,6 +106,10 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vla_paged_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(size)]
     lib.vla_paged_attention.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp, f32, vp, i64, vp,
                                         vp, size, vp]
+    lib.vla_kv_append_f8.argtypes = [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, i32, vp, vp]
+    lib.vla_kv_read_f8.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp]
+    lib.vla_paged_attention_f8.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, i32, vp, f32, vp,
+                                           i64, vp, vp, size, vp]
     lib.vla_prompt_attention.argtypes = [i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, f32, vp, i64, vp, vp]
     lib.vla_prompt_attention_backward_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(size)]
     lib.vla_prompt_attention_backward.argtypes = [i32, i32, i32, i32, i32, i32, vp, i64, vp, i64, vp, i64, vp, i64, vp, vp,
@@ -724,6 +728,80 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
         workspace = paged_attention_workspace(q, k_pages, page_table)
     n_ws = workspace.shape[0]
     _launch(index, lib.vla_paged_attention, n, H, K, hd, dt, qp, qs, pk, pv, n_pages, table, ld, max_pages,
+            _at(lens, torch.int32, index, "lens", n), scale, op, os_, _at(lse, torch.float32, index, "lse", n, H),
+            _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
+    return out
+
+
+
+def _pool_f8(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, index: int,
+             head_dim: int):
+    """Addresses of a cache of 8-bit numbers and of its scales, its pages and their key heads."""
+    f8 = torch.float8_e4m3fn
+    pk, pv, n, h = _pool(k_pages, v_pages, f8, index, head_dim)
+    shape = (n, h, CACHE_PAGE)
+    return (pk, pv, _at(k_scales, torch.float32, index, "k_scales", *shape),
+            _at(v_scales, torch.float32, index, "v_scales", *shape), n, h)
+
+
+def kv_append_f8(k: torch.Tensor, v: torch.Tensor, row_slot: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor,
+                 k_scales: torch.Tensor, v_scales: torch.Tensor) -> None:
+    """k and v [rows, n_kv_heads, head_dim] into slots row_slot of a cache of 8-bit numbers (vla_kv_append_f8): pages
+    float8_e4m3fn [n_pages, n_kv_heads, 16, head_dim] and [n_pages, n_kv_heads, head_dim, 16], scales fp32 [n_pages,
+    n_kv_heads, 16]."""
+    lib = _lib or load_library()
+    rows, K, hd, dt, index = _heads(k, "k")
+    kp, ks = _head_rows(k, k.dtype, index, "k", rows, K, hd)
+    vp, vs = _head_rows(v, k.dtype, index, "v", rows, K, hd)
+    pk, pv, sk, sv, n_pages, heads = _pool_f8(k_pages, v_pages, k_scales, v_scales, index, hd)
+    if heads != K:
+        raise ValueError("the pages must have the heads of k")
+    if rows == 0:
+        return
+    _launch(index, lib.vla_kv_append_f8, rows, K, hd, dt, kp, ks, vp, vs, pk, pv, sk, sv, n_pages,
+            _at(row_slot, torch.int32, index, "row_slot", rows))
+
+
+def kv_read_f8(row_slot: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor,
+               v_scales: torch.Tensor, dtype=torch.bfloat16, k_out: Optional[torch.Tensor] = None,
+               v_out: Optional[torch.Tensor] = None):
+    """(k, v) [rows, n_kv_heads, head_dim] of `dtype` (k_out's, if passed in) from slots row_slot of a cache of 8-bit numbers
+    (vla_kv_read_f8).  Rows whose slot lies outside are left as they were (of an output allocated here: zeros)."""
+    lib = _lib or load_library()
+    index, rows = row_slot.get_device(), row_slot.shape[0]
+    if index < 0 or k_pages.dim() != 4:
+        raise ValueError("row_slot must be a device tensor, k_pages [n_pages, n_kv_heads, 16, head_dim]")
+    hd = k_pages.shape[3]
+    pk, pv, sk, sv, n_pages, K = _pool_f8(k_pages, v_pages, k_scales, v_scales, index, hd)
+    if k_out is None:
+        k_out = torch.zeros((rows, K, hd), dtype=dtype, device=k_pages.device)
+    if v_out is None:
+        v_out = torch.zeros((rows, K, hd), dtype=k_out.dtype, device=k_pages.device)
+    dt = _heads(k_out, "k_out")[3]
+    kp, ks = _head_rows(k_out, k_out.dtype, index, "k_out", rows, K, hd)
+    vp, vs = _head_rows(v_out, k_out.dtype, index, "v_out", rows, K, hd)
+    if rows > 0:
+        _launch(index, lib.vla_kv_read_f8, rows, K, hd, dt, pk, pv, sk, sv, n_pages,
+                _at(row_slot, torch.int32, index, "row_slot", rows), kp, ks, vp, vs)
+    return k_out, v_out
+
+
+def paged_attention_f8(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor,
+                       v_scales: torch.Tensor, page_table: torch.Tensor, lens: torch.Tensor, scale: float,
+                       out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                       workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """paged_attention over a cache of 8-bit numbers (vla_paged_attention_f8); workspace: paged_attention_workspace's."""
+    lib = _lib or load_library()
+    n, H, hd, dt, index = _heads(q, "q")
+    dtype = q.dtype
+    out, op, os_ = _out_rows(out, q, index, "out", n, H, hd)
+    qp, qs = _head_rows(q, dtype, index, "q", n, H, hd)
+    pk, pv, sk, sv, n_pages, K = _pool_f8(k_pages, v_pages, k_scales, v_scales, index, hd)
+    table, ld, max_pages = _table(page_table, index, n)
+    if workspace is None:
+        workspace = paged_attention_workspace(q, k_pages, page_table)
+    n_ws = workspace.shape[0]
+    _launch(index, lib.vla_paged_attention_f8, n, H, K, hd, dt, qp, qs, pk, pv, sk, sv, n_pages, table, ld, max_pages,
             _at(lens, torch.int32, index, "lens", n), scale, op, os_, _at(lse, torch.float32, index, "lse", n, H),
             _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
     return out
