@@ -193,6 +193,31 @@ int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int3
                         float scale, void* out, int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes,
                         void* stream);
 
+/* vla_paged_attention where groups of environments begin with the same pages
+ * (continuations sampled from one observation and prompt, policies that share
+ * a long history): those are read once for a group.  Group g is environments
+ * group_start[g] .. group_start[g + 1] - 1, whose tables' first
+ * shared_pages[g] entries are alike, and whose lengths are 16 shared_pages[g]
+ * or more, or 0; the entries that are read are those of the group's first
+ * environment.  Arguments and results otherwise as vla_paged_attention's, but
+ * that the weights of shared pages are rounded once to `dtype`, that infinite
+ * and NaN elements there arrive as an infinity or as NaN, which is left open,
+ * and that an environment shorter than its group's pages gets NaN.
+ *   group_start   int32 [n_groups + 1], ascending from 0 or more to n_env or
+ *                 less; environments of no group share nothing (where it does
+ *                 not ascend, the results are left open)
+ *   shared_pages  int32 [n_groups]: below 0 counts as 0, above max_pages as it
+ *   workspace     vla_shared_attention_workspace_size bytes, 256-byte aligned
+ * n_groups at most 65535.  Where groups have fewer than two environments in
+ * the mean, nothing is gained, and nothing is shared. */
+int vla_shared_attention_workspace_size(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads,
+                                        int32_t head_dim, int32_t max_pages, size_t* bytes_host);
+int vla_shared_attention(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                         int32_t dtype, const void* q, int64_t ld_q, const void* k_pages, const void* v_pages,
+                         int32_t n_pages, const int32_t* page_table, int64_t ld_table, int32_t max_pages,
+                         const int32_t* lens, const int32_t* group_start, const int32_t* shared_pages, float scale,
+                         void* out, int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes, void* stream);
+
 /* ---- the cache in 8-bit numbers ----
  * Half the bytes of the pages above: the same pages with elements of one byte
  * (sign, 4 bits of exponent, 3 of mantissa; largest 448, no infinities, 0x7f

@@ -99,6 +99,16 @@ size_t paged_attn_bytes(int n_env, int n_heads, int n_kv_heads, int head_dim, in
 hipError_t launch_paged_attn(const PagedAttnArgs& a, hipStream_t s);
 hipError_t launch_paged_attn_f8(const PagedAttnArgs& a, hipStream_t s);  // pages of 8-bit numbers
 
+// The same where groups of environments share their first pages (vla_shared_attention).
+struct SharedArgs {
+  PagedAttnArgs a;
+  int n_groups;
+  const int32_t* group_start;   // [n_groups + 1]
+  const int32_t* shared_pages;  // [n_groups]
+};
+size_t shared_attn_bytes(int n_env, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_pages);
+hipError_t launch_shared_attn(const SharedArgs& s, hipStream_t stream);
+
 // Keys and values into pages of 8-bit numbers, and back (vla_kv_append_f8, vla_kv_read_f8).
 struct KvF8Args {
   int rows, n_kv_heads, head_dim;

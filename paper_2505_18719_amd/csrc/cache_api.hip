@@ -3,6 +3,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <cstdio>
 
 #include "cache.h"
 #include "cache_checks.h"
@@ -185,8 +186,8 @@ int vla_paged_attention_workspace_size(int32_t n_env, int32_t n_heads, int32_t n
   return set_error(VLA_OK, "");
 }
 
-// What the attentions over pages of either kind check alike.
-static int check_paged(const PagedAttnArgs& a, int64_t workspace_bytes) {
+// What the attentions over pages check alike; `need`: bytes of the workspace that `size_call` says.
+static int check_paged(const PagedAttnArgs& a, size_t workspace_bytes, size_t need, const char* size_call) {
   int rc = check_attention(a.n_env, a.n_heads, a.n_kv_heads, a.head_dim, a.max_pages);
   if (rc == VLA_OK) rc = check_heads(a.n_heads, a.n_kv_heads, a.head_dim, a.type);
   if (rc != VLA_OK) return rc;
@@ -199,10 +200,18 @@ static int check_paged(const PagedAttnArgs& a, int64_t workspace_bytes) {
   if (!a.lens || (a.max_pages > 0 && !a.page_table) || (a.n_pages > 0 && (!a.pages.k || !a.pages.v)))
     return set_error(VLA_EINVAL, "NULL argument");
   if (!aligned(a.pages.k) || !aligned(a.pages.v)) return set_error(VLA_EINVAL, "pages must start on 16 bytes");
-  const size_t need = paged_attn_bytes(a.n_env, a.n_heads, a.n_kv_heads, a.head_dim, a.max_pages);
-  if (need > 0 && (!a.ws || !aligned(a.ws, 256) || (size_t)workspace_bytes < need))
-    return set_error(VLA_EWORKSPACE, "workspace smaller than vla_paged_attention_workspace_size() or misaligned");
+  if (need > 0 && (!a.ws || !aligned(a.ws, 256) || workspace_bytes < need)) {
+    char msg[128];
+    std::snprintf(msg, sizeof msg, "workspace smaller than %s() or misaligned", size_call);
+    return set_error(VLA_EWORKSPACE, msg);
+  }
   return VLA_OK;
+}
+static int check_paged(const PagedAttnArgs& a, size_t workspace_bytes) {
+  const int rc = check_attention(a.n_env, a.n_heads, a.n_kv_heads, a.head_dim, a.max_pages);
+  if (rc != VLA_OK) return rc;
+  return check_paged(a, workspace_bytes, paged_attn_bytes(a.n_env, a.n_heads, a.n_kv_heads, a.head_dim, a.max_pages),
+                     "vla_paged_attention_workspace_size");
 }
 
 int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t dtype,
@@ -234,6 +243,42 @@ int vla_paged_attention_f8(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, i
   if (n_env == 0) return set_error(VLA_OK, "");
   if (n_pages > 0 && (!k_scales || !v_scales)) return set_error(VLA_EINVAL, "NULL argument");
   return hip_status("vla_paged_attention_f8", launch_paged_attn_f8(a, static_cast<hipStream_t>(stream)));
+}
+
+static int check_shared(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_pages) {
+  const int rc = check_attention(n_env, n_heads, n_kv_heads, head_dim, max_pages);
+  if (rc != VLA_OK) return rc;
+  if (n_groups < 0) return set_error(VLA_EINVAL, "negative size");
+  if (n_groups > 65535) return set_error(VLA_EUNSUPPORTED, "at most 65535 groups");
+  return VLA_OK;
+}
+
+int vla_shared_attention_workspace_size(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads,
+                                        int32_t head_dim, int32_t max_pages, size_t* bytes_host) {
+  if (!bytes_host) return set_error(VLA_EINVAL, "NULL argument");
+  const int rc = check_shared(n_env, n_groups, n_heads, n_kv_heads, head_dim, max_pages);
+  if (rc != VLA_OK) return rc;
+  *bytes_host = shared_attn_bytes(n_env, n_groups, n_heads, n_kv_heads, head_dim, max_pages);
+  return set_error(VLA_OK, "");
+}
+
+int vla_shared_attention(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                         int32_t dtype, const void* q, int64_t ld_q, const void* k_pages, const void* v_pages,
+                         int32_t n_pages, const int32_t* page_table, int64_t ld_table, int32_t max_pages,
+                         const int32_t* lens, const int32_t* group_start, const int32_t* shared_pages, float scale,
+                         void* out, int64_t ld_o, float* lse, void* workspace, size_t workspace_bytes, void* stream) {
+  const SharedArgs s{{n_env, n_heads, n_kv_heads, head_dim, static_cast<CacheType>(dtype), static_cast<const bf16_t*>(q),
+                      ld_q, {static_cast<bf16_t*>(const_cast<void*>(k_pages)), static_cast<bf16_t*>(const_cast<void*>(v_pages))},
+                      n_pages, page_table, ld_table, max_pages, lens, scale, static_cast<bf16_t*>(out), ld_o, lse, workspace,
+                      nullptr, nullptr}, n_groups, group_start, shared_pages};
+  int rc = check_shared(n_env, n_groups, n_heads, n_kv_heads, head_dim, max_pages);
+  if (rc != VLA_OK) return rc;
+  rc = check_paged(s.a, workspace_bytes, n_env == 0 ? 0 : shared_attn_bytes(n_env, n_groups, n_heads, n_kv_heads, head_dim, max_pages),
+                   "vla_shared_attention_workspace_size");
+  if (rc != VLA_OK) return rc;
+  if (n_env == 0) return set_error(VLA_OK, "");
+  if (n_groups > 0 && (!group_start || !shared_pages)) return set_error(VLA_EINVAL, "NULL argument");
+  return hip_status("vla_shared_attention", launch_shared_attn(s, static_cast<hipStream_t>(stream)));
 }
 
 static int check_kv_f8(const KvF8Args& a) {

@@ -932,7 +932,7 @@ __global__ __launch_bounds__(kJoinThreads) void attn_join_piece_kernel(PagedAttn
 }
 
 // ------------------------------------------------------------------ host
-int query_rows(int group, int tiles) { return std::min(16 * tiles, group); }
+inline int query_rows(int group, int tiles) { return std::min(16 * tiles, group); }
 
 template <int HD, CacheType T, int QT, bool STREAM, int W>
 hipError_t launch_whole(const PagedAttnArgs& a, int blocks, int rows, hipStream_t s) {
@@ -971,7 +971,7 @@ hipError_t launch_run(const PagedAttnArgs& a, int blocks, int rows, hipStream_t 
 // 18.2 / 26.1; 16 of up to 1024, 128 pieces, 12.8 / 15.3; but 8 x 1024, 64 pieces, 18.2 / 14.5).  Beyond, the split is about as
 // fast where pieces abound (64 x 4096, 512 pieces, 169 / 172.5) and faster where they are few or uneven (1 x 1024, 8 pieces, 12.0 /
 // 9.8; 8 x 3000, 8 pieces, 29.6 / 11.4; 64 of up to 2048 56.5 / 54.0).
-bool split_keys(long long pieces, int max_pages) { return max_pages > (pieces >= 128 ? 64 : 32); }
+inline bool split_keys(long long pieces, int max_pages) { return max_pages > (pieces >= 128 ? 64 : 32); }
 
 template <int HD, CacheType T, int QT, bool STREAM>
 hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
@@ -986,7 +986,7 @@ hipError_t launch_blocks(const PagedAttnArgs& a, hipStream_t s) {
 
 // Query heads of a group by tiles of 16: up to head_dim 128 two share a step's keys in registers (at 256 two tiles' sums do
 // not fit), further ones read the keys again.
-int query_tiles(int group, int head_dim) { return head_dim < 256 && group > 16 ? 2 : 1; }
+inline int query_tiles(int group, int head_dim) { return head_dim < 256 && group > 16 ? 2 : 1; }
 
 // A pool of up to 32 MB, the L2s' size, may be in the caches from one step to the next (278 tokens, 32 key heads: 6.3 us with
 // cached loads; in a larger pool, past the caches, 7.9); beyond, reads past the caches are faster (64 x 4096: 191 and 173 us).

@@ -17,82 +17,7 @@
 namespace vla {
 namespace {
 
-template <int HD, CacheType T>
-struct Queries {
-  static constexpr int KS = HD / 16, MB = HD / 32;
-  uint4 q[KS];
-  f32x16 o[MB];
-  float m, l;   // of this lane's query: largest score, this lane's part of the weights' sum
-  float scale;  // ScoreScale's
-
-  __device__ __forceinline__ void load(const bf16_t* row, float s) {
-    const int h = (threadIdx.x & 63) >> 5;
-    const ScoreScale sc(s);
-#pragma unroll
-    for (int i = 0; i < KS; ++i) q[i] = sc.turned(*reinterpret_cast<const uint4*>(row + 16 * i + 8 * h));
-    scale = sc.base2;
-    m = -INFINITY;
-    l = 0.f;
-#pragma unroll
-    for (int i = 0; i < MB; ++i) o[i] = zeros16();
-  }
-
-  // s = scores of the tile's keys
-  __device__ __forceinline__ void scores(const TileLane<HD>& at, const char* k, f32x16 (&s)[2]) {
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      s[t] = zeros16();
-#pragma unroll
-      for (int i = 0; i < KS; ++i) s[t] = mma32<T>(at.rows(k, 32 * t, i), q[i], s[t]);
-    }
-  }
-  // Scores of keys behind `last` (from the tile's first) count as -inf.
-  __device__ __forceinline__ void mask(f32x16 (&s)[2], int last) {
-    const int h = (threadIdx.x & 63) >> 5;
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r)
-        if (32 * t + mma_row(r, h) > last) s[t][r] = -INFINITY;
-  }
-  // s = weights under the new maximum; l and o follow it
-  __device__ __forceinline__ void weigh(f32x16 (&s)[2]) {
-    float mx = fmaxf(s[0][0], s[1][0]);
-#pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fmaxf(s[0][r], s[1][r]));
-    mx = fmaxf(m, half_max(mx));
-    if (__any(mx > m)) {
-      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mx) * scale);
-      l *= c;
-#pragma unroll
-      for (int i = 0; i < MB; ++i) o[i] *= c;
-      m = mx;
-    }
-    const float base = (m == -INFINITY ? 0.f : m * scale) - kWeightExp<T>;
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale, -base));
-        sum[r & 1] += s[t][r];
-      }
-    l += sum[0] + sum[1];
-  }
-  __device__ __forceinline__ void add(const TileLane<HD>& at, const char* v, const f32x16 (&s)[2]) {
-#pragma unroll
-    for (int b = 0; b < 4; ++b) {
-      const f32x16& p = s[b >> 1];
-      const int r = 8 * (b & 1);
-      // rounded to the type: 2^-9 (2^-12 in half precision) of a weight at most, of either sign, where the output's own rounding
-      // is as much of their weighted mean
-      const uint4 w = make_uint4(pack2<T>(p[r], p[r + 1]), pack2<T>(p[r + 2], p[r + 3]), pack2<T>(p[r + 4], p[r + 5]),
-                                 pack2<T>(p[r + 6], p[r + 7]));
-#pragma unroll
-      for (int i = 0; i < MB; ++i) o[i] = mma32<T>(at.cols(v, b, i), w, o[i]);
-    }
-  }
-};
+using namespace tiles;
 
 template <int HD, CacheType T, int NW>
 __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_attn_kernel(PromptArgs a) {
@@ -126,13 +51,13 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_attn_kernel
     if (j <= own) {
       f32x16 s[2];
       w.scores(at, tile(j, 0), s);
-      if (j == own) w.mask(s, qi - kTile * j);
+      if (j == own) w.template mask<false>(s, qi - kTile * j);
       w.weigh(s);
       w.add(at, tile(j, 1), s);
       if (j == own && __builtin_expect(any_nan(w.o), 0)) {  // a masked value may have spoiled the sums: once more without it
         const float m = w.m, l = w.l;
         w.scores(at, tile(j, 0), s);
-        w.mask(s, qi - kTile * j);
+        w.template mask<false>(s, qi - kTile * j);
         w.weigh(s);
         w.m = m;
         w.l = l;
@@ -186,7 +111,7 @@ hipError_t launch_type(const PromptArgs& a, hipStream_t s) {
 }  // namespace
 
 bool prompt_fits(int rows, int n_seq, int n_heads) {  // the smallest workgroups have 64 rows, none more than 512 threads
-  return n_seq < 1 << 26 && seq_items(rows, n_seq, 64) * n_heads * 512 < 1ll << 32;
+  return n_seq < 1 << 26 && tiles::seq_items(rows, n_seq, 64) * n_heads * 512 < 1ll << 32;
 }
 
 hipError_t launch_prompt_attn(const PromptArgs& a, hipStream_t s) {

@@ -17,6 +17,8 @@
 namespace vla {
 namespace {
 
+using namespace tiles;
+
 // Of a query: its log-sum-exp to base 2 (+inf where it has no score above -inf: all weights 0), and D.
 struct RowStat {
   float lse, d;

@@ -11,6 +11,7 @@
 #include "common.h"
 
 namespace vla {
+namespace tiles {
 
 constexpr int kTile = 64;  // rows of a tile in LDS
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
@@ -80,16 +81,24 @@ __device__ __forceinline__ int swz(int R) {
 template <int HD>
 constexpr int kTileBytes = kTile * HD * 2;
 
+// Rows of four pages of a cache as a tile: MFMA row m is the pages' token page_row(m), so that lane half h holds tokens 8 h .. 8 h + 7
+// of page b in registers 8 b .. 8 b + 7, which meet the 16 bytes of a feature's values there as they lie.
+__device__ __forceinline__ constexpr int page_row(int m) { return (m & 19) | (m >> 2 & 1) << 3 | (m >> 3 & 1) << 2; }
+
 // Lane addresses into a tile.
-template <int HD>
+template <int HD, bool PAGES = false>
 struct TileLane {
-  uint32_t row;   // chunk 0 of row lane % 32, before its place is turned
+  uint32_t row;   // chunk 0 of the lane's row, before its place is turned
   uint32_t turn;  // 16 (lane / 32 ^ swz of that row)
-  uint32_t col;   // first transposed read of features 0 .. 31
+  uint32_t col;   // first transposed read of features 0 .. 31; PAGES: this lane's feature of the first 32 in a page
   __device__ __forceinline__ TileLane() {
-    const int lane = threadIdx.x & 63, h = lane >> 5, i = lane & 15;
-    row = (lane & 31) * HD * 2;
-    turn = 16 * (h ^ swz<HD>(lane & 31));
+    const int lane = threadIdx.x & 63, h = lane >> 5, i = lane & 15, m = PAGES ? page_row(lane & 31) : lane & 31;
+    row = m * HD * 2;
+    turn = 16 * (h ^ swz<HD>(m));
+    if constexpr (PAGES) {
+      col = 32 * (lane & 31) + 16 * h;
+      return;
+    }
     const int r = 4 * h + (i >> 2);
     col = r * HD * 2 + 16 * ((2 * (lane >> 4 & 1) + (i >> 1 & 1)) ^ swz<HD>(r)) + 8 * (i & 1);
   }
@@ -97,8 +106,10 @@ struct TileLane {
   __device__ __forceinline__ uint4 rows(const char* tile, int r0, int ks) const {
     return *reinterpret_cast<const uint4*>(tile + r0 * HD * 2 + row + (turn ^ 32 * ks));
   }
-  // Features 32 mb + lane % 32, rows 16 b + 4 (lane / 32) .. + 4 and 8 more on.
+  // Features 32 mb + lane % 32, rows 16 b + 4 (lane / 32) .. + 4 and 8 more on; PAGES: of page b's values [HD][16], tokens
+  // 8 (lane / 32) .. + 8.
   __device__ __forceinline__ uint4 cols(const char* tile, int b, int mb) const {
+    if constexpr (PAGES) return *reinterpret_cast<const uint4*>(tile + (b * HD + 32 * mb) * 32 + col);
     // eight rows on, bit 1 of the place turns; 32 features on, bits 2 and up
     const char* p = tile + 16 * b * HD * 2;
     return __builtin_bit_cast(uint4, lds_read_tr(p + (col ^ 64 * mb), p + 8 * HD * 2 + (col ^ 32 ^ 64 * mb)));
@@ -188,6 +199,87 @@ __device__ __forceinline__ void store_row(bf16_t* row, const f32x16 (&acc)[HD / 
     }
 }
 
+// ------------------------------------------------------------------ 32 queries of a wave
+template <int HD, CacheType T>
+struct Queries {
+  static constexpr int KS = HD / 16, MB = HD / 32;
+  uint4 q[KS];
+  f32x16 o[MB];
+  float m, l;   // of this lane's query: largest score, this lane's part of the weights' sum
+  float scale;  // ScoreScale's
+
+  __device__ __forceinline__ void load(const bf16_t* row, float s) {
+    const int h = (threadIdx.x & 63) >> 5;
+    const ScoreScale sc(s);
+#pragma unroll
+    for (int i = 0; i < KS; ++i) q[i] = sc.turned(*reinterpret_cast<const uint4*>(row + 16 * i + 8 * h));
+    scale = sc.base2;
+    m = -INFINITY;
+    l = 0.f;
+#pragma unroll
+    for (int i = 0; i < MB; ++i) o[i] = zeros16();
+  }
+
+  // s = scores of the tile's keys
+  template <bool PAGES>
+  __device__ __forceinline__ void scores(const TileLane<HD, PAGES>& at, const char* k, f32x16 (&s)[2]) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      s[t] = zeros16();
+#pragma unroll
+      for (int i = 0; i < KS; ++i) s[t] = mma32<T>(at.rows(k, 32 * t, i), q[i], s[t]);
+    }
+  }
+  // Scores of keys behind `last` (from the tile's first) count as -inf.
+  template <bool PAGES>
+  __device__ __forceinline__ void mask(f32x16 (&s)[2], int last) {
+    const int h = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        if (32 * t + (PAGES ? page_row(mma_row(r, h)) : mma_row(r, h)) > last) s[t][r] = -INFINITY;
+  }
+  // s = weights under the new maximum; l and o follow it
+  __device__ __forceinline__ void weigh(f32x16 (&s)[2]) {
+    float mx = fmaxf(s[0][0], s[1][0]);
+#pragma unroll
+    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fmaxf(s[0][r], s[1][r]));
+    mx = fmaxf(m, half_max(mx));
+    if (__any(mx > m)) {
+      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mx) * scale);
+      l *= c;
+#pragma unroll
+      for (int i = 0; i < MB; ++i) o[i] *= c;
+      m = mx;
+    }
+    const float base = (m == -INFINITY ? 0.f : m * scale) - kWeightExp<T>;
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int t = 0; t < 2; ++t)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale, -base));
+        sum[r & 1] += s[t][r];
+      }
+    l += sum[0] + sum[1];
+  }
+  template <bool PAGES>
+  __device__ __forceinline__ void add(const TileLane<HD, PAGES>& at, const char* v, const f32x16 (&s)[2]) {
+#pragma unroll
+    for (int b = 0; b < 4; ++b) {
+      const f32x16& p = s[b >> 1];
+      const int r = 8 * (b & 1);
+      // rounded to the type: 2^-9 (2^-12 in half precision) of a weight at most, of either sign, where the output's own rounding
+      // is as much of their weighted mean
+      const uint4 w = make_uint4(pack2<T>(p[r], p[r + 1]), pack2<T>(p[r + 2], p[r + 3]), pack2<T>(p[r + 4], p[r + 5]),
+                                 pack2<T>(p[r + 6], p[r + 7]));
+#pragma unroll
+      for (int i = 0; i < MB; ++i) o[i] = mma32<T>(at.cols(v, b, i), w, o[i]);
+    }
+  }
+};
+
 // ------------------------------------------------------------------ from a workgroup to its rows
 // Sequence s has items row_start[s] / M + s and on, one per M of its rows begun: enough of them, and none of the next sequence's,
 // whatever the lengths, so that a workgroup finds its sequence by a search of row_start; the items in between are empty.
@@ -220,4 +312,5 @@ __device__ __forceinline__ bool find_tile(const int32_t* row_start, int n_seq, i
   return true;
 }
 
+}  // namespace tiles
 }  // namespace vla

@@ -28,7 +28,7 @@ EXPORTS = ("vla_workspace_size", "vla_create", "vla_prefill", "vla_decode_action
            "vla_last_error", "vla_extract_actions", "vla_gae", "vla_ppo_clip", "vla_logprob_backward",
            "vla_train_workspace_size", "vla_ppo_lora_grads", "vla_kv_plan", "vla_rope_freqs", "vla_qk_norm_rope",
            "vla_qk_norm_rope_workspace_size", "vla_qk_norm_rope_backward", "vla_paged_attention_workspace_size",
-           "vla_paged_attention", "vla_kv_append_f8", "vla_kv_read_f8", "vla_paged_attention_f8", "vla_prompt_attention", "vla_prompt_attention_backward_workspace_size",
+           "vla_paged_attention", "vla_shared_attention_workspace_size", "vla_shared_attention", "vla_kv_append_f8", "vla_kv_read_f8", "vla_paged_attention_f8", "vla_prompt_attention", "vla_prompt_attention_backward_workspace_size",
            "vla_prompt_attention_backward")
 # projections a LoRA adapter merges into (VLA_PROJ_* order), by weight-dict key
 PROJECTIONS = ("wq", "wk", "wv", "wo", "wgate", "wup", "wdown")
@@ -106,6 +106,9 @@ def load_library(path: str = LIB_PATH) -> ctypes.CDLL:
     lib.vla_paged_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, ctypes.POINTER(size)]
     lib.vla_paged_attention.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp, f32, vp, i64, vp,
                                         vp, size, vp]
+    lib.vla_shared_attention_workspace_size.argtypes = [i32, i32, i32, i32, i32, i32, ctypes.POINTER(size)]
+    lib.vla_shared_attention.argtypes = [i32, i32, i32, i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp, vp, vp, f32, vp,
+                                         i64, vp, vp, size, vp]
     lib.vla_kv_append_f8.argtypes = [i32, i32, i32, i32, vp, i64, vp, i64, vp, vp, vp, vp, i32, vp, vp]
     lib.vla_kv_read_f8.argtypes = [i32, i32, i32, i32, vp, vp, vp, vp, i32, vp, vp, i64, vp, i64, vp]
     lib.vla_paged_attention_f8.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, i32, vp, f32, vp,
@@ -732,6 +735,42 @@ def paged_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tenso
             _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
     return out
 
+
+
+def shared_attention_workspace(q: torch.Tensor, k_pages: torch.Tensor, page_table: torch.Tensor,
+                               group_start: torch.Tensor) -> torch.Tensor:
+    """The workspace of shared_attention for calls of these shapes."""
+    lib = load_library()
+    n = ctypes.c_size_t()
+    _check(lib.vla_shared_attention_workspace_size(q.shape[0], group_start.shape[0] - 1, q.shape[1], k_pages.shape[1],
+                                                   q.shape[2], page_table.shape[1], ctypes.byref(n)))
+    return torch.empty(n.value, dtype=torch.uint8, device=q.device)
+
+
+def shared_attention(q: torch.Tensor, k_pages: torch.Tensor, v_pages: torch.Tensor, page_table: torch.Tensor,
+                     lens: torch.Tensor, group_start: torch.Tensor, shared_pages: torch.Tensor, scale: float,
+                     out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None,
+                     workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """paged_attention of environments that come in groups group_start[g] .. group_start[g + 1] - 1, int32 [n_groups + 1],
+    whose first shared_pages[g] pages, int32 [n_groups], are alike and read once for the group (vla_shared_attention)."""
+    lib = _lib or load_library()
+    n, H, hd, dt, index = _heads(q, "q")
+    dtype = q.dtype
+    out, op, os_ = _out_rows(out, q, index, "out", n, H, hd)
+    qp, qs = _head_rows(q, dtype, index, "q", n, H, hd)
+    pk, pv, n_pages, K = _pool(k_pages, v_pages, dtype, index, hd)
+    table, ld, max_pages = _table(page_table, index, n)
+    groups = group_start.shape[0] - 1 if group_start.dim() == 1 else -1
+    if groups < 0:
+        raise ValueError("group_start must be [n_groups + 1]")
+    if workspace is None:
+        workspace = shared_attention_workspace(q, k_pages, page_table, group_start)
+    n_ws = workspace.shape[0]
+    _launch(index, lib.vla_shared_attention, n, groups, H, K, hd, dt, qp, qs, pk, pv, n_pages, table, ld, max_pages,
+            _at(lens, torch.int32, index, "lens", n), _at(group_start, torch.int32, index, "group_start", groups + 1),
+            _at(shared_pages, torch.int32, index, "shared_pages", groups), scale, op, os_,
+            _at(lse, torch.float32, index, "lse", n, H), _at(workspace, torch.uint8, index, "workspace", n_ws), n_ws)
+    return out
 
 
 def _pool_f8(k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor, index: int,
