@@ -38,46 +38,75 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_attn_kernel
   const TileLane<HD> at;
   const int last = (min(M * (st.tile + 1), st.len) - 1) / kTile;  // tile of the workgroup's last query
   const int own = q0 < st.len ? q0 / kTile : -1;                  // of this wave's queries
-  auto tile = [&](int j, int which) { return lds + (2 * (j & 1) + which) * kTileBytes<HD>; };
-  copy_tile<HD, NW>(tile(last, 0), k, kTile * last, st.len, wave);
-  copy_tile<HD, NW>(tile(last, 1), v, kTile * last, st.len, wave);
-  WAIT_VMCNT(0);
-  __syncthreads();
-  for (int j = last; j >= 0; --j) {
-    if (j > 0) {
-      copy_tile<HD, NW>(tile(j - 1, 0), k, kTile * (j - 1), st.len, wave);
-      copy_tile<HD, NW>(tile(j - 1, 1), v, kTile * (j - 1), st.len, wave);
-    }
-    if (j <= own) {
-      f32x16 s[2];
-      w.scores(at, tile(j, 0), s);
-      if (j == own) w.template mask<false>(s, qi - kTile * j);
-      w.weigh(s);
-      w.add(at, tile(j, 1), s);
-      if (j == own && __builtin_expect(any_nan(w.o), 0)) {  // a masked value may have spoiled the sums: once more without it
-        const float m = w.m, l = w.l;
-        w.scores(at, tile(j, 0), s);
-        w.template mask<false>(s, qi - kTile * j);
-        w.weigh(s);
-        w.m = m;
-        w.l = l;
-#pragma unroll
-        for (int i = 0; i < HD / 32; ++i) w.o[i] = zeros16();
-#pragma unroll
-        for (int t = 0; t < 2; ++t) add_apart<HD, T>(w.o, s[t], tile(j, 1), 32 * t, [&](int key) { return kTile * j + key <= qi; });
-      }
-    }
+  auto keys = [&](int j) { return lds + (j & 1) * kTileBytes<HD>; };
+  auto values = [&](int j) { return lds + (2 + (j & 1)) * kTileBytes<HD>; };
+  auto copy_keys = [&](int j) { if (j >= 0) copy_tile<HD, NW>(keys(j), k, kTile * j, st.len, wave); };
+  auto copy_values = [&](int j) { if (j >= 0) copy_tile<HD, NW>(values(j), v, kTile * j, st.len, wave); };
+  auto arrived = [&] {
     WAIT_VMCNT(0);
     __syncthreads();
+  };
+  // Scores are a tile ahead of the weights, so that the matrix units have the next ones' products while the vector units take the
+  // weights: at tile j its scores are there, as are keys j - 1 and values j in LDS, and keys j - 2 and values j - 1 are on their way.
+  f32x16 s[2];
+  copy_keys(last);
+  copy_values(last);
+  copy_keys(last - 1);
+  arrived();
+  if (own == last) w.scores(at, keys(last), s);
+  __syncthreads();
+  int j = last;
+  for (; j > own; --j) {  // tiles of the workgroup's later queries only
+    copy_keys(j - 2);
+    copy_values(j - 1);
+    if (j - 1 == own) w.scores(at, keys(own), s);
+    arrived();
+  }
+  if (own < 0) return;
+  copy_keys(j - 2);
+  copy_values(j - 1);
+  w.template mask<false>(s, qi - kTile * j);
+  w.follow(s);
+  {
+    f32x16 p[2] = {s[0], s[1]};
+    w.weigh(p);
+    w.add(at, values(j), p);
+  }
+  if (__builtin_expect(any_nan(w.o), 0)) {  // a masked value may have spoiled the sums: once more without it
+    const float l = w.l;
+    w.weigh(s);
+    w.l = l;
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i) w.o[i] = zeros16();
+#pragma unroll
+    for (int t = 0; t < 2; ++t) add_apart<HD, T>(w.o, s[t], values(j), 32 * t, [&](int key) { return kTile * j + key <= qi; });
+  }
+  if (j > 0) w.scores(at, keys(j - 1), s);
+  arrived();
+  for (--j; j > 0; --j) {
+    copy_keys(j - 2);
+    copy_values(j - 1);
+    w.follow(s);
+    f32x16 next[2];
+    w.scores(at, keys(j - 1), next);
+    w.weigh(s);
+    w.add(at, values(j), s);
+    s[0] = next[0];
+    s[1] = next[1];
+    arrived();
+  }
+  if (j == 0) {
+    w.follow(s);
+    w.weigh(s);
+    w.add(at, values(0), s);
   }
   const float l = half_sum(w.l), r = l == 0.f ? 0.f : 1.f / l;
-  if (own < 0) return;
   if (l == 0.f) {  // no score above -inf: zeros whatever the values
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) w.o[i] = zeros16();
   }
   store_row<HD, T>(a.o.p + row * a.o.ld + head * HD, w.o, r, mine);
-  if (a.lse && mine && lane < 32) a.lse[row * a.n_heads + head] = ((w.m * w.scale - kWeightExp<T>) + __builtin_amdgcn_logf(l)) * kLn2;
+  if (a.lse && mine && lane < 32) a.lse[row * a.n_heads + head] = ((w.m * w.scale - kHeldExp<T>) + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <int HD, CacheType T, int NW>
@@ -94,8 +123,6 @@ hipError_t launch(const PromptArgs& a, hipStream_t s) {
 template <int HD, CacheType T>
 hipError_t launch_rows(const PromptArgs& a, hipStream_t s) {
   auto groups = [&](int waves) { return seq_items(a.rows, a.n_seq, 32 * waves) * a.n_heads; };
-  if constexpr (HD < 256)
-    if (groups(8) >= 512) return launch<HD, T, 8>(a, s);
   if (groups(4) >= 512) return launch<HD, T, 4>(a, s);
   return launch<HD, T, 2>(a, s);
 }

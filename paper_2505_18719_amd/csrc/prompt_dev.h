@@ -18,6 +18,8 @@ constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 template <CacheType T>
 __device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, const f32x16& c) {
@@ -27,8 +29,9 @@ __device__ __forceinline__ f32x16 mma32(const uint4& a, const uint4& b, const f3
 // Two numbers of the type, to nearest even.
 template <CacheType T>
 __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
-  if constexpr (T == kBf16) return pack2bf(lo, hi);
-  else return __builtin_bit_cast(uint32_t, (f16x2){(_Float16)lo, (_Float16)hi});
+  const f32x2 v = {lo, hi};  // as a pair: one conversion of both
+  if constexpr (T == kBf16) return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, bf16x2));
+  else return __builtin_bit_cast(uint32_t, __builtin_convertvector(v, f16x2));
 }
 template <CacheType T>
 __device__ __forceinline__ float2 unpack2(uint32_t v) {
@@ -51,6 +54,11 @@ struct ScoreScale {
 // below 2^-29 of the largest.
 template <CacheType T>
 constexpr float kWeightExp = T == kBf16 ? 0.f : 15.f;
+// The running maximum follows the scores only where they pass it by a factor of 2^4 of the weights: 17 products of what is summed per
+// tile are saved at most of them.  Weights are then up to 16, and half-precision ones held 2^11 times as large.
+constexpr float kSlack = 4.f;
+template <CacheType T>
+constexpr float kHeldExp = T == kBf16 ? 0.f : kWeightExp<T> - kSlack;
 __device__ __forceinline__ f32x16 zeros16() {
   f32x16 z;
 #pragma unroll
@@ -240,20 +248,24 @@ struct Queries {
       for (int r = 0; r < 16; ++r)
         if (32 * t + (PAGES ? page_row(mma_row(r, h)) : mma_row(r, h)) > last) s[t][r] = -INFINITY;
   }
-  // s = weights under the new maximum; l and o follow it
-  __device__ __forceinline__ void weigh(f32x16 (&s)[2]) {
-    float mx = fmaxf(s[0][0], s[1][0]);
+  // The maximum follows scores that pass it by kSlack, and l and o the maximum.
+  __device__ __forceinline__ void follow(const f32x16 (&s)[2]) {
+    float mx = __builtin_elementwise_maximum(s[0][0], s[1][0]);
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = fmaxf(mx, fmaxf(s[0][r], s[1][r]));
-    mx = fmaxf(m, half_max(mx));
-    if (__any(mx > m)) {
-      const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mx) * scale);
+    for (int r = 1; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(s[0][r], s[1][r]));
+    mx = half_max(mx);
+    const bool passed = (mx - m) * scale > kSlack || (m == -INFINITY && mx > m);
+    if (__any(passed)) {
+      const float c = !passed ? 1.f : m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((m - mx) * scale);
       l *= c;
 #pragma unroll
       for (int i = 0; i < MB; ++i) o[i] *= c;
-      m = mx;
+      m = passed ? mx : m;
     }
-    const float base = (m == -INFINITY ? 0.f : m * scale) - kWeightExp<T>;
+  }
+  // s = weights under the maximum
+  __device__ __forceinline__ void weigh(f32x16 (&s)[2]) {
+    const float base = (m == -INFINITY ? 0.f : m * scale) - kHeldExp<T>;
     float sum[2] = {0.f, 0.f};
 #pragma unroll
     for (int t = 0; t < 2; ++t)

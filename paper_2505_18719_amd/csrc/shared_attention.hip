@@ -136,6 +136,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void attn_shared_kernel
       f32x16 s[2];
       w.scores(at, tile(j, 0), s);
       if (kPage * pages - kTile * j < kTile) w.template mask<true>(s, kPage * pages - 1 - kTile * j);
+      w.follow(s);
       w.weigh(s);
       w.add(at, tile(j, 1), s);
     }
@@ -150,7 +151,8 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void attn_shared_kernel
   if (col >= n_col) return;
   const float l = any_bad ? __builtin_nanf("") : half_sum(w.l);
   const size_t to = part * sp.columns + (size_t)env * a.n_heads + head;
-  if (lane < 32) sp.ml[to] = make_float2(w.m == -INFINITY ? -INFINITY : w.m * w.scale, l);
+  // in half precision the weights are held at another power of two than those of the own pages
+  if (lane < 32) sp.ml[to] = make_float2(w.m == -INFINITY ? -INFINITY : w.m * w.scale + (kWeightExp<T> - tiles::kHeldExp<T>), l);
   float* o = sp.o + to * HD + 4 * (lane >> 5);
 #pragma unroll
   for (int mb = 0; mb < HD / 32; ++mb)
