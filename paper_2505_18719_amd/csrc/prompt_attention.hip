@@ -9,6 +9,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cstdlib>
 
 #include "lds_limit.h"
 #include "prompt.h"
@@ -19,59 +20,62 @@ namespace {
 
 using namespace tiles;
 
-template <int HD, CacheType T, int NW>
-__global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_attn_kernel(PromptArgs a) {
+// Waves that a SIMD is to hold: 3 have 168 registers each, 2 have 256, 1 has 512.
+template <int HD>
+constexpr int kWavesPerSimd = HD == 256 ? 1 : HD == 64 ? 3 : 2;
+
+template <int HD, CacheType T, int NW, int KT>
+__global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel(PromptArgs a) {
   extern __shared__ __align__(16) char lds[];
-  constexpr int M = 32 * NW;
-  const int head = blockIdx.x % a.n_heads, item = blockIdx.x / a.n_heads;
-  SeqTile st;
-  if (!find_tile<M>(a.row_start, a.n_seq, a.rows, item, st)) return;
+  const int kvh = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads, group = a.n_heads / a.n_kv_heads;
+  SeqItem st;
+  if (!find_item<NW>(a.row_start, a.n_seq, a.rows, group, item, st)) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = head / (a.n_heads / a.n_kv_heads);
   const SeqRows k = {a.k.p + st.row0 * a.k.ld + kvh * HD, a.k.ld}, v = {a.v.p + st.row0 * a.v.ld + kvh * HD, a.v.ld};
-  const int q0 = M * st.tile + 32 * wave;  // this wave's first query
+  const int line = NW * st.nth + wave;  // this wave's place in the sequence's line
+  const int q0 = 32 * (line / group), head = kvh * group + line % group;
   const int qi = q0 + (lane & 31);
   const bool mine = qi < st.len;
   const int64_t row = st.row0 + (int64_t)min(qi, st.len - 1);
-  Queries<HD, T> w;
+  Queries<HD, T, KT> w;
   w.load(a.q.p + row * a.q.ld + head * HD, a.scale);
   const TileLane<HD> at;
-  const int last = (min(M * (st.tile + 1), st.len) - 1) / kTile;  // tile of the workgroup's last query
-  const int own = q0 < st.len ? q0 / kTile : -1;                  // of this wave's queries
-  auto keys = [&](int j) { return lds + (j & 1) * kTileBytes<HD>; };
-  auto values = [&](int j) { return lds + (2 + (j & 1)) * kTileBytes<HD>; };
-  auto copy_keys = [&](int j) { if (j >= 0) copy_tile<HD, NW>(keys(j), k, kTile * j, st.len, wave); };
-  auto copy_values = [&](int j) { if (j >= 0) copy_tile<HD, NW>(values(j), v, kTile * j, st.len, wave); };
+  const int last = (min(32 * ((NW * (st.nth + 1) - 1) / group) + 32, st.len) - 1) / KT;  // tile of the workgroup's last query
+  const int own = q0 < st.len ? q0 / KT : -1;                                          // of this wave's queries
+  // Buffers by the parity of the tile, at places that the loop over pairs of tiles knows beforehand.
+  auto keys = [&](int parity) { return lds + parity * kTileBytes<HD, KT>; };
+  auto values = [&](int parity) { return lds + (2 + parity) * kTileBytes<HD, KT>; };
+  auto copy_keys = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW, KT>(keys(parity), k, KT * j, st.len, wave); };
+  auto copy_values = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW, KT>(values(parity), v, KT * j, st.len, wave); };
   auto arrived = [&] {
     WAIT_VMCNT(0);
     __syncthreads();
   };
   // Scores are a tile ahead of the weights, so that the matrix units have the next ones' products while the vector units take the
   // weights: at tile j its scores are there, as are keys j - 1 and values j in LDS, and keys j - 2 and values j - 1 are on their way.
-  f32x16 s[2];
-  copy_keys(last);
-  copy_values(last);
-  copy_keys(last - 1);
+  typename Queries<HD, T, KT>::Scores s, next;
+  copy_keys(last, last & 1);
+  copy_values(last, last & 1);
+  copy_keys(last - 1, ~last & 1);
   arrived();
-  if (own == last) w.scores(at, keys(last), s);
+  if (own == last) w.scores(at, keys(last & 1), s);
   __syncthreads();
   int j = last;
   for (; j > own; --j) {  // tiles of the workgroup's later queries only
-    copy_keys(j - 2);
-    copy_values(j - 1);
-    if (j - 1 == own) w.scores(at, keys(own), s);
+    copy_keys(j - 2, j & 1);
+    copy_values(j - 1, ~j & 1);
+    if (j - 1 == own) w.scores(at, keys(~j & 1), s);
     arrived();
   }
   if (own < 0) return;
-  copy_keys(j - 2);
-  copy_values(j - 1);
-  w.template mask<false>(s, qi - kTile * j);
+  copy_keys(j - 2, j & 1);
+  copy_values(j - 1, ~j & 1);
+  w.template mask<false>(s, qi - KT * j);
   w.follow(s);
-  {
-    f32x16 p[2] = {s[0], s[1]};
-    w.weigh(p);
-    w.add(at, values(j), p);
-  }
+#pragma unroll
+  for (int t = 0; t < KT / 32; ++t) next[t] = s[t];
+  w.weigh(next);
+  w.add(at, values(j & 1), next);
   if (__builtin_expect(any_nan(w.o), 0)) {  // a masked value may have spoiled the sums: once more without it
     const float l = w.l;
     w.weigh(s);
@@ -79,21 +83,28 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_attn_kernel
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) w.o[i] = zeros16();
 #pragma unroll
-    for (int t = 0; t < 2; ++t) add_apart<HD, T>(w.o, s[t], values(j), 32 * t, [&](int key) { return kTile * j + key <= qi; });
+    for (int t = 0; t < KT / 32; ++t) add_apart<HD, T>(w.o, s[t], values(j & 1), 32 * t, [&](int key) { return KT * j + key <= qi; });
   }
-  if (j > 0) w.scores(at, keys(j - 1), s);
+  if (j > 0) w.scores(at, keys(~j & 1), s);
   arrived();
-  for (--j; j > 0; --j) {
-    copy_keys(j - 2);
-    copy_values(j - 1);
+  auto tile = [&](int j, int parity, typename Queries<HD, T, KT>::Scores& s, typename Queries<HD, T, KT>::Scores& next) {
+    copy_keys(j - 2, parity);
+    copy_values(j - 1, 1 - parity);
     w.follow(s);
-    f32x16 next[2];
-    w.scores(at, keys(j - 1), next);
+    w.scores(at, keys(1 - parity), next);
     w.weigh(s);
-    w.add(at, values(j), s);
-    s[0] = next[0];
-    s[1] = next[1];
+    w.add(at, values(parity), s);
     arrived();
+  };
+  if (--j > 0 && j % 2 == 1) {
+    tile(j, 1, s, next);
+#pragma unroll
+    for (int t = 0; t < KT / 32; ++t) s[t] = next[t];
+    --j;
+  }
+  for (; j > 0; j -= 2) {
+    tile(j, 0, s, next);
+    tile(j - 1, 1, next, s);
   }
   if (j == 0) {
     w.follow(s);
@@ -109,22 +120,29 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_attn_kernel
   if (a.lse && mine && lane < 32) a.lse[row * a.n_heads + head] = ((w.m * w.scale - kHeldExp<T>) + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int HD, CacheType T, int NW>
+template <int HD, CacheType T, int NW, int KT>
 hipError_t launch(const PromptArgs& a, hipStream_t s) {
   static LdsLimit limit;
-  const auto kernel = prompt_attn_kernel<HD, T, NW>;
-  const hipError_t e = limit.allow((const void*)kernel, 4 * kTileBytes<HD>);
+  const auto kernel = prompt_attn_kernel<HD, T, NW, KT>;
+  constexpr int kLds = 4 * kTileBytes<HD, KT>;
+  const hipError_t e = limit.allow((const void*)kernel, kLds);
   if (e != hipSuccess) return e;
-  const long long groups = seq_items(a.rows, a.n_seq, 32 * NW) * a.n_heads;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * NW), 4 * kTileBytes<HD>, s, a);
+  const long long groups = seq_items<NW>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * NW), kLds, s, a);
   return hipGetLastError();
 }
 
 template <int HD, CacheType T>
 hipError_t launch_rows(const PromptArgs& a, hipStream_t s) {
-  auto groups = [&](int waves) { return seq_items(a.rows, a.n_seq, 32 * waves) * a.n_heads; };
-  if (groups(4) >= 512) return launch<HD, T, 4>(a, s);
-  return launch<HD, T, 2>(a, s);
+  if (const char* e = getenv("VLA_NW")) {
+    const int w = atoi(e);
+    if (w == 4) return launch<HD, T, 4, 64>(a, s);
+    if (w == 2) return launch<HD, T, 2, 64>(a, s);
+    if (w == 24) return launch<HD, T, 4, 32>(a, s);
+    return launch<HD, T, 2, 32>(a, s);
+  }
+  if (seq_items<4>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads >= 512) return launch<HD, T, 4, 64>(a, s);
+  return launch<HD, T, 2, 32>(a, s);
 }
 
 template <CacheType T>
@@ -137,8 +155,8 @@ hipError_t launch_type(const PromptArgs& a, hipStream_t s) {
 
 }  // namespace
 
-bool prompt_fits(int rows, int n_seq, int n_heads) {  // the smallest workgroups have 64 rows, none more than 512 threads
-  return n_seq < 1 << 26 && tiles::seq_items(rows, n_seq, 64) * n_heads * 512 < 1ll << 32;
+bool prompt_fits(int rows, int n_seq, int n_heads) {  // threads of the most workgroups that there can be, of two waves
+  return n_seq < 1 << 26 && (tiles::seq_items<2>(rows, n_seq, 1) + n_seq) * n_heads * 128 < 1ll << 32;
 }
 
 hipError_t launch_prompt_attn(const PromptArgs& a, hipStream_t s) {

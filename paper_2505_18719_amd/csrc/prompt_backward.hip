@@ -80,12 +80,12 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   constexpr int M = 32 * NW, KS = HD / 16;
   const PromptArgs& a = b.fwd;
   const int head = blockIdx.x % a.n_heads, item = blockIdx.x / a.n_heads;
-  SeqTile st;
-  if (!find_tile<M>(a.row_start, a.n_seq, a.rows, item, st)) return;
+  SeqItem st;
+  if (!find_item<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kvh = head / (a.n_heads / a.n_kv_heads);
   const SeqRows k = {a.k.p + st.row0 * a.k.ld + kvh * HD, a.k.ld}, v = {a.v.p + st.row0 * a.v.ld + kvh * HD, a.v.ld};
-  const int q0 = M * st.tile + 32 * wave, qi = q0 + (lane & 31);
+  const int q0 = M * st.nth + 32 * wave, qi = q0 + (lane & 31);
   const bool mine = qi < st.len;
   const int64_t row = st.row0 + (int64_t)min(qi, st.len - 1);
   const ScoreScale sc(a.scale);
@@ -110,7 +110,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   Column<HD, T> dq;
   dq.begin();
   const TileLane<HD> at;
-  const int last = (min(M * (st.tile + 1), st.len) - 1) / kTile, own = q0 < st.len ? q0 / kTile : -1;
+  const int last = (min(M * (st.nth + 1), st.len) - 1) / kTile, own = q0 < st.len ? q0 / kTile : -1;
   auto tile = [&](int j, int which) { return lds + (2 * (j & 1) + which) * kTileBytes<HD>; };
   // dS of the 32 keys from 32 t on of tile j, before the scale
   auto ds_of = [&](int j, int t, bool masked) {
@@ -174,10 +174,10 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
   constexpr int M = 32 * NW, KS = HD / 16;
   const PromptArgs& a = b.fwd;
   const int kvh = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads, group = a.n_heads / a.n_kv_heads;
-  SeqTile st;
-  if (!find_tile<M>(a.row_start, a.n_seq, a.rows, item, st)) return;
+  SeqItem st;
+  if (!find_item<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int k0 = M * st.tile + 32 * wave, kj = k0 + (lane & 31);
+  const int k0 = M * st.nth + 32 * wave, kj = k0 + (lane & 31);
   const bool mine = kj < st.len;
   const int64_t row = st.row0 + (int64_t)min(kj, st.len - 1);
   const ScoreScale sc(a.scale);
@@ -189,8 +189,8 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
   }
   Column<HD, T> dk, dv;
   const TileLane<HD> at;
-  const int first = M * st.tile / kTile, end = (st.len + kTile - 1) / kTile;        // tiles of queries
-  const int last_own = (min(M * (st.tile + 1), st.len) - 1) / kTile;                // of the workgroup's last key
+  const int first = M * st.nth / kTile, end = (st.len + kTile - 1) / kTile;        // tiles of queries
+  const int last_own = (min(M * (st.nth + 1), st.len) - 1) / kTile;                // of the workgroup's last key
   const int own = k0 < st.len ? k0 / kTile : end;                                   // of this wave's keys: the one with masked pairs
   auto tile = [&](int n, int which) { return lds + (2 * (n & 1) + which) * kTileBytes<HD>; };
   auto stat = [&](int n) { return reinterpret_cast<float2*>(lds + 4 * kTileBytes<HD>) + (n & 1) * kTile; };
@@ -305,7 +305,7 @@ hipError_t launch(const PromptBwdArgs& b, hipStream_t s) {
   hipError_t e = dq_limit.allow((const void*)dq, kDq);
   if (e == hipSuccess) e = dkv_limit.allow((const void*)dkv, kDkv);
   if (e != hipSuccess) return e;
-  const long long items = seq_items(b.fwd.rows, b.fwd.n_seq, 32 * NW);
+  const long long items = seq_items<NW>(b.fwd.rows, b.fwd.n_seq, 1);
   float2* stats = static_cast<float2*>(b.ws);
   hipLaunchKernelGGL(dq, dim3((unsigned)(items * b.fwd.n_heads)), dim3(64 * NW), kDq, s, b, stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -13,7 +13,7 @@
 namespace vla {
 namespace tiles {
 
-constexpr int kTile = 64;  // rows of a tile in LDS
+constexpr int kTile = 64;  // rows of a tile in LDS, where a kernel does not say otherwise
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -86,8 +86,8 @@ template <int HD>
 __device__ __forceinline__ int swz(int R) {
   return HD == 64 ? ((R >> 1 & 1) << 2 | (R >> 2 & 3)) : ((R & 3) << 2 | (R >> 2 & 3));
 }
-template <int HD>
-constexpr int kTileBytes = kTile * HD * 2;
+template <int HD, int KT = kTile>
+constexpr int kTileBytes = KT * HD * 2;
 
 // Rows of four pages of a cache as a tile: MFMA row m is the pages' token page_row(m), so that lane half h holds tokens 8 h .. 8 h + 7
 // of page b in registers 8 b .. 8 b + 7, which meet the 16 bytes of a feature's values there as they lie.
@@ -129,11 +129,11 @@ struct SeqRows {
   const bf16_t* p;
   int64_t ld;
 };
-// Copies rows r0 .. r0 + 63 of a sequence of `len` rows into a tile (rows behind its last: that one), 1 KB per wave and
+// Copies rows r0 .. r0 + KT - 1 of a sequence of `len` rows into a tile (rows behind its last: that one), 1 KB per wave and
 // instruction; the waves of the workgroup share them.
-template <int HD, int NW>
+template <int HD, int NW, int KT = kTile>
 __device__ __forceinline__ void copy_tile(char* tile, const SeqRows& x, int r0, int len, int wave) {
-  constexpr int CH = HD / 8, RPK = 64 / CH, N = kTile / RPK;  // chunks of a row, rows of a copy, copies
+  constexpr int CH = HD / 8, RPK = 64 / CH, N = KT / RPK;  // chunks of a row, rows of a copy, copies
   const int lane = threadIdx.x & 63;
   const uint32_t lb = (uint32_t)(uintptr_t)((lds_ptr_t*)tile);
   const __amdgpu_buffer_rsrc_t rs =
@@ -143,7 +143,7 @@ __device__ __forceinline__ void copy_tile(char* tile, const SeqRows& x, int r0, 
     const int j = i * NW + wave;
     if (N % NW != 0 && j >= N) break;
     const int R = j * RPK + lane / CH;
-    lds_dma16(lb + j * 1024, (uint32_t)(min(R, len - 1 - r0) * (int)x.ld + 8 * ((lane % CH) ^ swz<HD>(R))) * 2, rs, 0);
+    lds_dma16(__builtin_amdgcn_readfirstlane(lb + j * 1024), (uint32_t)(min(R, len - 1 - r0) * (int)x.ld + 8 * ((lane % CH) ^ swz<HD>(R))) * 2, rs, 0);
   }
 }
 
@@ -208,9 +208,10 @@ __device__ __forceinline__ void store_row(bf16_t* row, const f32x16 (&acc)[HD / 
 }
 
 // ------------------------------------------------------------------ 32 queries of a wave
-template <int HD, CacheType T>
+template <int HD, CacheType T, int KT = kTile>
 struct Queries {
-  static constexpr int KS = HD / 16, MB = HD / 32;
+  static constexpr int KS = HD / 16, MB = HD / 32, N = KT / 32;  // steps of the products with keys, blocks of features, of keys
+  typedef f32x16 Scores[N];
   uint4 q[KS];
   f32x16 o[MB];
   float m, l;   // of this lane's query: largest score, this lane's part of the weights' sum
@@ -230,9 +231,9 @@ struct Queries {
 
   // s = scores of the tile's keys
   template <bool PAGES>
-  __device__ __forceinline__ void scores(const TileLane<HD, PAGES>& at, const char* k, f32x16 (&s)[2]) {
+  __device__ __forceinline__ void scores(const TileLane<HD, PAGES>& at, const char* k, Scores& s) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < N; ++t) {
       s[t] = zeros16();
 #pragma unroll
       for (int i = 0; i < KS; ++i) s[t] = mma32<T>(at.rows(k, 32 * t, i), q[i], s[t]);
@@ -240,19 +241,19 @@ struct Queries {
   }
   // Scores of keys behind `last` (from the tile's first) count as -inf.
   template <bool PAGES>
-  __device__ __forceinline__ void mask(f32x16 (&s)[2], int last) {
+  __device__ __forceinline__ void mask(Scores& s, int last) {
     const int h = (threadIdx.x & 63) >> 5;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r)
         if (32 * t + (PAGES ? page_row(mma_row(r, h)) : mma_row(r, h)) > last) s[t][r] = -INFINITY;
   }
   // The maximum follows scores that pass it by kSlack, and l and o the maximum.
-  __device__ __forceinline__ void follow(const f32x16 (&s)[2]) {
-    float mx = __builtin_elementwise_maximum(s[0][0], s[1][0]);
+  __device__ __forceinline__ void follow(const Scores& s) {
+    float mx = s[0][0];
 #pragma unroll
-    for (int r = 1; r < 16; ++r) mx = __builtin_elementwise_maximum(mx, __builtin_elementwise_maximum(s[0][r], s[1][r]));
+    for (int r = 1; r < 16 * N; ++r) mx = __builtin_elementwise_maximum(mx, s[r / 16][r % 16]);
     mx = half_max(mx);
     const bool passed = (mx - m) * scale > kSlack || (m == -INFINITY && mx > m);
     if (__any(passed)) {
@@ -264,11 +265,11 @@ struct Queries {
     }
   }
   // s = weights under the maximum
-  __device__ __forceinline__ void weigh(f32x16 (&s)[2]) {
+  __device__ __forceinline__ void weigh(Scores& s) {
     const float base = (m == -INFINITY ? 0.f : m * scale) - kHeldExp<T>;
     float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
         s[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], scale, -base));
@@ -277,9 +278,9 @@ struct Queries {
     l += sum[0] + sum[1];
   }
   template <bool PAGES>
-  __device__ __forceinline__ void add(const TileLane<HD, PAGES>& at, const char* v, const f32x16 (&s)[2]) {
+  __device__ __forceinline__ void add(const TileLane<HD, PAGES>& at, const char* v, const Scores& s) {
 #pragma unroll
-    for (int b = 0; b < 4; ++b) {
+    for (int b = 0; b < 2 * N; ++b) {
       const f32x16& p = s[b >> 1];
       const int r = 8 * (b & 1);
       // rounded to the type: 2^-9 (2^-12 in half precision) of a weight at most, of either sign, where the output's own rounding
@@ -293,35 +294,44 @@ struct Queries {
 };
 
 // ------------------------------------------------------------------ from a workgroup to its rows
-// Sequence s has items row_start[s] / M + s and on, one per M of its rows begun: enough of them, and none of the next sequence's,
-// whatever the lengths, so that a workgroup finds its sequence by a search of row_start; the items in between are empty.
-struct SeqTile {
-  int row0, len, tile;  // first row and rows of the sequence, the item's M rows
+// A wave takes a block of 32 rows of one of `group` heads: a sequence's blocks and heads lie in a line, block by block, of which
+// a workgroup takes NW, so that its waves have keys alike, and none idles but for a sequence's last item.  Sequence s has items
+// first_item(row_start[s], s) and on: enough of them, and none of the next sequence's, whatever the lengths, so that a workgroup
+// finds its sequence by a search of row_start; the items in between are empty.
+struct SeqItem {
+  int row0, len, nth;  // first row and rows of the sequence, the item's place in it from the last one back
 };
-inline __host__ __device__ long long seq_items(int rows, int n_seq, int M) { return (long long)rows / M + n_seq; }
+template <int NW>
+__host__ __device__ __forceinline__ long long first_item(int start, int s, int group) {
+  return ((long long)(start / 32) + s) * group / NW + s;
+}
+template <int NW>
+long long seq_items(int rows, int n_seq, int group) { return first_item<NW>(rows, n_seq, group); }
 
-template <int M>
-__device__ __forceinline__ bool find_tile(const int32_t* row_start, int n_seq, int rows, int item, SeqTile& t) {
+template <int NW>
+__device__ __forceinline__ bool find_item(const int32_t* row_start, int n_seq, int rows, int group, int item, SeqItem& t) {
   const int lane = threadIdx.x & 63;
-  int lo = 0, n = n_seq;
+  int lo = 0, n = n_seq, start, end;
   for (;;) {
-    const int step = (n + kWave - 1) / kWave, at = lo + lane * step;
-    const bool before = (long long)lane * step < n && min(max(row_start[min(at, n_seq)], 0), rows) / M + at <= item;
+    const int step = (n + kWave - 1) / kWave, at = min(lo + lane * step, n_seq), v = row_start[at];
+    const bool before = lane * step < n && first_item<NW>(min(max(v, 0), rows), at, group) <= item;
     const int found = __popcll(__ballot(before));
     if (found == 0) return false;
     lo += (found - 1) * step;
     n = min(step, n - (found - 1) * step);
-    if (step == 1) break;
+    if (step > 1) continue;
+    start = __builtin_amdgcn_readlane(v, found - 1);
+    end = found < kWave ? __builtin_amdgcn_readlane(v, found) : row_start[min(lo + 1, n_seq)];
+    break;
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  t.row0 = __builtin_amdgcn_readfirstlane(row_start[lo]);
-  const int end = __builtin_amdgcn_readfirstlane(row_start[lo + 1]);
+  t.row0 = __builtin_amdgcn_readfirstlane(start);
+  end = __builtin_amdgcn_readfirstlane(end);
   if (t.row0 < 0 || end <= t.row0 || end > rows) return false;
   t.len = end - t.row0;
-  const int tiles = (t.len + M - 1) / M, nth = item - (t.row0 / M + lo);
-  if (nth >= tiles) return false;
-  t.tile = tiles - 1 - nth;  // the longest rows of a sequence first
-  return true;
+  const int items = (int)(((long long)((t.len + 31) / 32) * group + NW - 1) / NW);
+  const int nth = item - (int)first_item<NW>(t.row0, __builtin_amdgcn_readfirstlane(lo), group);
+  t.nth = items - 1 - nth;  // the longest rows of a sequence first
+  return nth < items;
 }
 
 }  // namespace tiles
