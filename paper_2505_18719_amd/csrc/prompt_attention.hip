@@ -9,7 +9,6 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
-#include <cstdlib>
 
 #include "lds_limit.h"
 #include "prompt.h"
@@ -24,7 +23,7 @@ using namespace tiles;
 template <int HD>
 constexpr int kWavesPerSimd = HD == 256 ? 1 : HD == 64 ? 3 : 2;
 
-template <int HD, CacheType T, int NW, int KT>
+template <int HD, CacheType T, int NW>
 __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel(PromptArgs a) {
   extern __shared__ __align__(16) char lds[];
   const int kvh = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads, group = a.n_heads / a.n_kv_heads;
@@ -37,23 +36,23 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
   const int qi = q0 + (lane & 31);
   const bool mine = qi < st.len;
   const int64_t row = st.row0 + (int64_t)min(qi, st.len - 1);
-  Queries<HD, T, KT> w;
+  Queries<HD, T> w;
   w.load(a.q.p + row * a.q.ld + head * HD, a.scale);
   const TileLane<HD> at;
-  const int last = (min(32 * ((NW * (st.nth + 1) - 1) / group) + 32, st.len) - 1) / KT;  // tile of the workgroup's last query
-  const int own = q0 < st.len ? q0 / KT : -1;                                          // of this wave's queries
+  const int last = (min(32 * ((NW * (st.nth + 1) - 1) / group) + 32, st.len) - 1) / kTile;  // tile of the workgroup's last query
+  const int own = q0 < st.len ? q0 / kTile : -1;                                          // of this wave's queries
   // Buffers by the parity of the tile, at places that the loop over pairs of tiles knows beforehand.
-  auto keys = [&](int parity) { return lds + parity * kTileBytes<HD, KT>; };
-  auto values = [&](int parity) { return lds + (2 + parity) * kTileBytes<HD, KT>; };
-  auto copy_keys = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW, KT>(keys(parity), k, KT * j, st.len, wave); };
-  auto copy_values = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW, KT>(values(parity), v, KT * j, st.len, wave); };
+  auto keys = [&](int parity) { return lds + parity * kTileBytes<HD>; };
+  auto values = [&](int parity) { return lds + (2 + parity) * kTileBytes<HD>; };
+  auto copy_keys = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW>(keys(parity), k, kTile * j, st.len, wave); };
+  auto copy_values = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW>(values(parity), v, kTile * j, st.len, wave); };
   auto arrived = [&] {
     WAIT_VMCNT(0);
     __syncthreads();
   };
   // Scores are a tile ahead of the weights, so that the matrix units have the next ones' products while the vector units take the
   // weights: at tile j its scores are there, as are keys j - 1 and values j in LDS, and keys j - 2 and values j - 1 are on their way.
-  typename Queries<HD, T, KT>::Scores s, next;
+  typename Queries<HD, T>::Scores s, next;
   copy_keys(last, last & 1);
   copy_values(last, last & 1);
   copy_keys(last - 1, ~last & 1);
@@ -70,10 +69,10 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
   if (own < 0) return;
   copy_keys(j - 2, j & 1);
   copy_values(j - 1, ~j & 1);
-  w.template mask<false>(s, qi - KT * j);
+  w.template mask<false>(s, qi - kTile * j);
   w.follow(s);
 #pragma unroll
-  for (int t = 0; t < KT / 32; ++t) next[t] = s[t];
+  for (int t = 0; t < kTile / 32; ++t) next[t] = s[t];
   w.weigh(next);
   w.add(at, values(j & 1), next);
   if (__builtin_expect(any_nan(w.o), 0)) {  // a masked value may have spoiled the sums: once more without it
@@ -83,11 +82,11 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) w.o[i] = zeros16();
 #pragma unroll
-    for (int t = 0; t < KT / 32; ++t) add_apart<HD, T>(w.o, s[t], values(j & 1), 32 * t, [&](int key) { return KT * j + key <= qi; });
+    for (int t = 0; t < kTile / 32; ++t) add_apart<HD, T>(w.o, s[t], values(j & 1), 32 * t, [&](int key) { return kTile * j + key <= qi; });
   }
   if (j > 0) w.scores(at, keys(~j & 1), s);
   arrived();
-  auto tile = [&](int j, int parity, typename Queries<HD, T, KT>::Scores& s, typename Queries<HD, T, KT>::Scores& next) {
+  auto tile = [&](int j, int parity, typename Queries<HD, T>::Scores& s, typename Queries<HD, T>::Scores& next) {
     copy_keys(j - 2, parity);
     copy_values(j - 1, 1 - parity);
     w.follow(s);
@@ -99,7 +98,7 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
   if (--j > 0 && j % 2 == 1) {
     tile(j, 1, s, next);
 #pragma unroll
-    for (int t = 0; t < KT / 32; ++t) s[t] = next[t];
+    for (int t = 0; t < kTile / 32; ++t) s[t] = next[t];
     --j;
   }
   for (; j > 0; j -= 2) {
@@ -116,15 +115,17 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
 #pragma unroll
     for (int i = 0; i < HD / 32; ++i) w.o[i] = zeros16();
   }
-  store_row<HD, T>(a.o.p + row * a.o.ld + head * HD, w.o, r, mine);
+  __syncthreads();  // the tiles have been used
+  constexpr int kShare = 4 * kTileBytes<HD> / NW;
+  store_rows<HD, T, kShare>(lds + wave * kShare, a.o.p + (st.row0 + (int64_t)q0) * a.o.ld + head * HD, a.o.ld, min(st.len - q0, 32), w.o, r);
   if (a.lse && mine && lane < 32) a.lse[row * a.n_heads + head] = ((w.m * w.scale - kHeldExp<T>) + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int HD, CacheType T, int NW, int KT>
+template <int HD, CacheType T, int NW>
 hipError_t launch(const PromptArgs& a, hipStream_t s) {
   static LdsLimit limit;
-  const auto kernel = prompt_attn_kernel<HD, T, NW, KT>;
-  constexpr int kLds = 4 * kTileBytes<HD, KT>;
+  const auto kernel = prompt_attn_kernel<HD, T, NW>;
+  constexpr int kLds = 4 * kTileBytes<HD>;
   const hipError_t e = limit.allow((const void*)kernel, kLds);
   if (e != hipSuccess) return e;
   const long long groups = seq_items<NW>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads;
@@ -134,15 +135,10 @@ hipError_t launch(const PromptArgs& a, hipStream_t s) {
 
 template <int HD, CacheType T>
 hipError_t launch_rows(const PromptArgs& a, hipStream_t s) {
-  if (const char* e = getenv("VLA_NW")) {
-    const int w = atoi(e);
-    if (w == 4) return launch<HD, T, 4, 64>(a, s);
-    if (w == 2) return launch<HD, T, 2, 64>(a, s);
-    if (w == 24) return launch<HD, T, 4, 32>(a, s);
-    return launch<HD, T, 2, 32>(a, s);
-  }
-  if (seq_items<4>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads >= 512) return launch<HD, T, 4, 64>(a, s);
-  return launch<HD, T, 2, 32>(a, s);
+  // Four waves share a tile's way through LDS, two workgroups a CU (64 x 272 to 304 rows, 32 heads: 129 us, with two waves 181, with
+  // eight 148; 8190 rows, 28 heads: 493, 688 and 487); where those do not fill the GPU, two are as fast or faster (one of 278: 10.5 us, 10.8).
+  if (seq_items<4>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads >= 512) return launch<HD, T, 4>(a, s);
+  return launch<HD, T, 2>(a, s);
 }
 
 template <CacheType T>

@@ -13,7 +13,7 @@
 namespace vla {
 namespace tiles {
 
-constexpr int kTile = 64;  // rows of a tile in LDS, where a kernel does not say otherwise
+constexpr int kTile = 64;  // rows of a tile in LDS
 constexpr float kLog2e = 1.44269504088896340736f, kLn2 = 0.69314718055994530942f;
 
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
@@ -86,8 +86,8 @@ template <int HD>
 __device__ __forceinline__ int swz(int R) {
   return HD == 64 ? ((R >> 1 & 1) << 2 | (R >> 2 & 3)) : ((R & 3) << 2 | (R >> 2 & 3));
 }
-template <int HD, int KT = kTile>
-constexpr int kTileBytes = KT * HD * 2;
+template <int HD>
+constexpr int kTileBytes = kTile * HD * 2;
 
 // Rows of four pages of a cache as a tile: MFMA row m is the pages' token page_row(m), so that lane half h holds tokens 8 h .. 8 h + 7
 // of page b in registers 8 b .. 8 b + 7, which meet the 16 bytes of a feature's values there as they lie.
@@ -129,11 +129,11 @@ struct SeqRows {
   const bf16_t* p;
   int64_t ld;
 };
-// Copies rows r0 .. r0 + KT - 1 of a sequence of `len` rows into a tile (rows behind its last: that one), 1 KB per wave and
+// Copies rows r0 .. r0 + 63 of a sequence of `len` rows into a tile (rows behind its last: that one), 1 KB per wave and
 // instruction; the waves of the workgroup share them.
-template <int HD, int NW, int KT = kTile>
+template <int HD, int NW>
 __device__ __forceinline__ void copy_tile(char* tile, const SeqRows& x, int r0, int len, int wave) {
-  constexpr int CH = HD / 8, RPK = 64 / CH, N = KT / RPK;  // chunks of a row, rows of a copy, copies
+  constexpr int CH = HD / 8, RPK = 64 / CH, N = kTile / RPK;  // chunks of a row, rows of a copy, copies
   const int lane = threadIdx.x & 63;
   const uint32_t lb = (uint32_t)(uintptr_t)((lds_ptr_t*)tile);
   const __amdgpu_buffer_rsrc_t rs =
@@ -207,10 +207,46 @@ __device__ __forceinline__ void store_row(bf16_t* row, const f32x16 (&acc)[HD / 
     }
 }
 
+// Writes the columns of acc, times each lane's `mul`, as `n` rows (at most 32) of HD numbers of the type: through BYTES of LDS of the
+// wave's own, so that a store writes whole rows (stores straight from the columns write 32 bytes of 32 rows).
+template <int HD, CacheType T, int BYTES>
+__device__ __forceinline__ void store_rows(char* lds, bf16_t* row, int64_t ld, int n, const f32x16 (&acc)[HD / 32], float mul) {
+  constexpr int F = BYTES / 64 < HD ? BYTES / 64 : HD, CH = F / 8, RPI = 64 / CH;  // features at a time, their 16-byte chunks, rows a store
+  static_assert(F % 32 == 0, "whole blocks of features");
+  const int lane = threadIdx.x & 63, h = lane >> 5, r = lane & 31;
+#pragma unroll
+  for (int f0 = 0; f0 < HD; f0 += F) {
+#pragma unroll
+    for (int mb = 0; mb < F / 32; ++mb)
+#pragma unroll
+      for (int i = 0; i < 4; i += 2) {
+        const f32x16& x = acc[f0 / 32 + mb];
+        uint32_t a[2], b[2];  // features 8 i + 4 h .. + 4, and eight on
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          a[e] = pack2<T>(x[4 * i + 2 * e] * mul, x[4 * i + 2 * e + 1] * mul);
+          b[e] = pack2<T>(x[4 * i + 4 + 2 * e] * mul, x[4 * i + 5 + 2 * e] * mul);
+        }
+        // lane half 0 gets features 8 i .. + 8, half 1 those eight on
+        const auto u = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
+        const auto v = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
+        *reinterpret_cast<uint4*>(lds + r * (F * 2) + 16 * ((4 * mb + i + h) ^ (r & (CH - 1)))) = make_uint4(u[0], v[0], u[1], v[1]);
+      }
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int k = 0; k < 32 / RPI; ++k) {
+      const int R = k * RPI + lane / CH, c = lane % CH;
+      const uint4 x = *reinterpret_cast<const uint4*>(lds + R * (F * 2) + 16 * (c ^ (R & (CH - 1))));
+      if (R < n) *reinterpret_cast<uint4*>(row + R * ld + f0 + 8 * c) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
 // ------------------------------------------------------------------ 32 queries of a wave
-template <int HD, CacheType T, int KT = kTile>
+template <int HD, CacheType T>
 struct Queries {
-  static constexpr int KS = HD / 16, MB = HD / 32, N = KT / 32;  // steps of the products with keys, blocks of features, of keys
+  static constexpr int KS = HD / 16, MB = HD / 32, N = kTile / 32;  // steps of the products with keys, blocks of features, of keys
   typedef f32x16 Scores[N];
   uint4 q[KS];
   f32x16 o[MB];
