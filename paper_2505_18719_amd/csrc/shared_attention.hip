@@ -1,12 +1,11 @@
 // Attention of one new token per environment where groups of environments share their first pages (vla_shared_attention).
 //
-// Bound: HBM and the matrix units: the shared keys and values once for a group, 4 head_dim flops a query and key.  Three parts:
-//   shared  a workgroup takes 32 columns a wave, a column being one query head of one environment of a group, over a run of the
-//           group's shared pages, which pass through LDS in tiles of four as in attention over whole prompts, and leaves its
-//           columns' maximum, sum of weights and sum of weighted values
-//   own     a workgroup takes an environment's remaining pages, as attention without sharing does, and joins the parts; where
-//           there are few environments, a run of them, and leaves another part
-//   join    then adds the parts
+// Bound: HBM and the matrix units: the shared keys and values once for a group, 4 head_dim flops a query and key.  One launch of two
+// kinds of workgroups, and a join:
+//   shared  takes 32 columns a wave, a column being one query head of one environment of a group, over a run of the group's shared
+//           pages, which pass through LDS in tiles of four as in attention over whole prompts
+//   own     takes an environment's remaining pages, or a run of them, as attention without sharing does
+// Each leaves its columns' maxima, sums of weights and sums of weighted values.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -19,8 +18,8 @@ namespace {
 
 struct Plan {
   bool share;      // else vla_paged_attention's kernels
-  int waves;       // of a workgroup of the shared part
   int parts, own;  // runs of the shared pages, and of an environment's own
+  int all() const { return parts + own; }
 };
 
 // The parts of all columns: sums of weighted values [part][environment][head][HD], maxima (to base 2) and sums of weights.
@@ -35,59 +34,56 @@ PartSpace part_space(void* ws, const PagedAttnArgs& a, int parts) {
   return {o, reinterpret_cast<float2*>(o + (size_t)parts * columns * a.head_dim), columns};
 }
 
-// Items of the groups, as seq_items: C columns each.
-template <int C>
-__device__ __forceinline__ bool find_group(const SharedArgs& s, int item, int group, int& e0, int& n_col, int& c0, int& pages) {
+// The last group g with key(g) <= x: its environments e0 .. e1 - 1 and shared pages, as far as they are usable.  Each lane looks at one
+// group of 64 at a time, at its pages together with its start.
+struct Group {
+  int g, e0, e1, pages;
+};
+template <class F>
+__device__ __forceinline__ bool find_group(const SharedArgs& s, long long x, F key, Group& out) {
   const int lane = threadIdx.x & 63;
   int lo = 0, n = s.n_groups;
-  auto first = [&](int g) { return (int)((long long)min(max(s.group_start[g], 0), s.a.n_env) * group / C) + g; };
   for (;;) {
-    const int step = (n + kWave - 1) / kWave, at = lo + lane * step;
-    const int found = __popcll(__ballot(lane * step < n && first(min(at, s.n_groups)) <= item));
+    const int step = (n + kWave - 1) / kWave, at = min(lo + lane * step, s.n_groups), start = s.group_start[at];
+    const int pages = s.shared_pages[min(at, s.n_groups - 1)];
+    const int found = __popcll(__ballot(lane * step < n && key(start, at) <= x));
     if (found == 0) return false;
     lo += (found - 1) * step;
     n = min(step, n - (found - 1) * step);
-    if (step == 1) break;
+    if (step > 1) continue;
+    out.g = __builtin_amdgcn_readfirstlane(lo);
+    out.e0 = __builtin_amdgcn_readlane(start, found - 1);
+    out.e1 = __builtin_amdgcn_readfirstlane(found < kWave ? __builtin_amdgcn_readlane(start, found) : s.group_start[min(lo + 1, s.n_groups)]);
+    out.pages = min(max(__builtin_amdgcn_readlane(pages, found - 1), 0), s.a.max_pages);
+    return out.e0 >= 0 && out.e1 > out.e0 && out.e1 <= s.a.n_env;
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  e0 = __builtin_amdgcn_readfirstlane(s.group_start[lo]);
-  const int e1 = __builtin_amdgcn_readfirstlane(s.group_start[lo + 1]);
-  if (e0 < 0 || e1 <= e0 || e1 > s.a.n_env) return false;
-  n_col = (e1 - e0) * group;
-  c0 = (item - first(lo)) * C;
-  pages = min(__builtin_amdgcn_readfirstlane(s.shared_pages[lo]), s.a.max_pages);
-  return c0 < n_col && pages > 0;
+}
+// Items of the groups, C columns each: group g has items first_of(group_start[g], g) and on, as many as it needs or more.
+template <int C>
+__device__ __forceinline__ long long first_of(const SharedArgs& s, int start, int g, int group) {
+  return (long long)min(max(start, 0), s.a.n_env) * group / C + g;
 }
 // Pages that environment env shares with its group.
 __device__ __forceinline__ int shared_of(const SharedArgs& s, int env) {
-  const int lane = threadIdx.x & 63;
-  int lo = 0, n = s.n_groups;
-  for (;;) {
-    const int step = (n + kWave - 1) / kWave, at = lo + lane * step;
-    const int found = __popcll(__ballot(lane * step < n && s.group_start[min(at, s.n_groups)] <= env));
-    if (found == 0) return 0;
-    lo += (found - 1) * step;
-    n = min(step, n - (found - 1) * step);
-    if (step == 1) break;
-  }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  const int e0 = s.group_start[lo], e1 = s.group_start[lo + 1];
-  if (e0 < 0 || e0 > env || e1 <= env || e1 > s.a.n_env) return 0;
-  return __builtin_amdgcn_readfirstlane(min(max(s.shared_pages[lo], 0), s.a.max_pages));
+  Group g;
+  const bool found = find_group(s, env, [](int start, int) { return start; }, g);
+  return found && g.e1 > env ? g.pages : 0;
 }
 
 __host__ __device__ __forceinline__ int run_of(int n, int parts) { return (n + parts - 1) / parts; }
 
 // ------------------------------------------------------------------ shared pages
 template <int HD, CacheType T, int NW>
-__global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void attn_shared_kernel(SharedArgs args, PartSpace sp, int parts) {
+__device__ __forceinline__ void shared_part(const SharedArgs& args, const PartSpace& sp, int parts, int block, char* lds) {
   using namespace tiles;
-  extern __shared__ __align__(16) char lds[];
   constexpr int C = 32 * NW, CH = HD / 8, RPK = 64 / CH, PK = kPage / RPK;  // chunks of a row, rows of a copy, copies of a page
   const PagedAttnArgs& a = args.a;
-  const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads, part = rest % parts, group = a.n_heads / a.n_kv_heads;
-  int e0, n_col, c0, pages;
-  if (!find_group<C>(args, rest / parts, group, e0, n_col, c0, pages)) return;
+  const int kvh = block % a.n_kv_heads, rest = block / a.n_kv_heads, part = rest % parts, item = rest / parts;
+  const int group = a.n_heads / a.n_kv_heads;
+  Group of;
+  if (!find_group(args, item, [&](int start, int g) { return first_of<C>(args, start, g, group); }, of)) return;
+  const int e0 = of.e0, n_col = (of.e1 - e0) * group, c0 = (int)(item - first_of<C>(args, e0, of.g, group)) * C, pages = of.pages;
+  if (c0 >= n_col || pages == 0) return;
   const int n_tiles = (pages + 3) / 4, run = run_of(n_tiles, parts), j0 = part * run, j1 = min(j0 + run, n_tiles);
   if (j0 >= j1) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -178,40 +174,6 @@ __device__ __forceinline__ Own own_of(const SharedArgs& s, int env) {
   return o;
 }
 
-// Four features from f on of one head: parts of the shared pages (n of them), parts of its own (from `first` on, m of them), and N
-// parts in LDS.
-template <int HD, CacheType T, int N>
-__device__ __forceinline__ void join_column(const PagedAttnArgs& a, const PartSpace& sp, int env, int head, int f, int n, int first, int m,
-                                            const Parts<HD>* ps, int h) {
-  const size_t at = (size_t)env * a.n_heads + head;
-  auto part = [&](int i) { return i < n ? i : first + i - n; };
-  float mx = -INFINITY;
-#pragma unroll
-  for (int u = 0; u < N; ++u) mx = fmaxf(mx, ps->ml[u * 2 * ps->rows + h]);
-  for (int i = 0; i < n + m; ++i) mx = fmaxf(mx, sp.ml[part(i) * sp.columns + at].x);
-  float l = 0.f;
-  f32x4 v = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-  for (int u = 0; u < N; ++u) {
-    const float mu = ps->ml[u * 2 * ps->rows + h], c = mu == -INFINITY ? 1.f : worth(mu, mx);
-    l = fmaf(ps->ml[(u * 2 + 1) * ps->rows + h], c, l);
-    const f32x4 o = *reinterpret_cast<const f32x4*>(ps->o + (size_t)(u * ps->rows + h) * (HD + 4) + f);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], c, v[e]);
-  }
-#pragma unroll 4
-  for (int i = 0; i < n + m; ++i) {
-    const size_t p = part(i) * sp.columns + at;
-    const float2 ml = sp.ml[p];
-    const float c = ml.x == -INFINITY ? 1.f : worth(ml.x, mx);
-    l = fmaf(ml.y, c, l);
-    const f32x4 o = *reinterpret_cast<const f32x4*>(sp.o + p * HD + f);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], c, v[e]);
-  }
-  store4<T>(a.o + env * a.ld_o + (size_t)head * HD + f, v, reciprocal(l));
-  if (a.lse && f == 0) a.lse[at] = log_sum<T>(mx, l);
-}
 // Runs of the shared pages that there are parts of.
 __device__ __forceinline__ int shared_parts(int skip, int parts) {
   const int n = (skip + 3) / 4;
@@ -226,18 +188,14 @@ __device__ __forceinline__ void fill_rows(const PagedAttnArgs& a, int env, int h
 }
 
 template <int HD, CacheType T, int QT, int W>
-__global__ __launch_bounds__(64 * W) void attn_own_kernel(SharedArgs args, PartSpace sp, int parts, int runs, int rows) {
-  extern __shared__ __align__(16) float own_lds[];
+__device__ __forceinline__ void own_part(const SharedArgs& args, const PartSpace& sp, int parts, int runs, int rows, int block, float* lds) {
   const PagedAttnArgs& a = args.a;
-  const int env = blockIdx.y, run = blockIdx.x % runs;
-  const HeadBlock b = head_block<QT>(a, blockIdx.x / runs);
+  const int blocks = head_blocks<QT>(a.n_heads / a.n_kv_heads) * a.n_kv_heads, run = block % runs, env = block / runs / blocks;
+  const HeadBlock b = head_block<QT>(a, block / runs % blocks);
   const Own own = own_of<T>(args, env);
-  if (own.zeros || own.bad) {
-    if (runs == 1) fill_rows<HD, T>(a, env, b.head0, b.n, own.zeros);
-    return;
-  }
+  if (own.steps == 0) return;
   const int per = run_of(own.steps, runs), s0 = run * per, s1 = min(s0 + per, own.steps);
-  if (runs > 1 && s0 >= s1) return;
+  if (s0 >= s1) return;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), max_pages = a.max_pages - own.skip;
   const int32_t* pt = a.page_table + env * a.ld_table + own.skip;
   Wave<HD, T, QT, false> wave(a);
@@ -283,15 +241,9 @@ __global__ __launch_bounds__(64 * W) void attn_own_kernel(SharedArgs args, PartS
       wave.end();
     }
   }
-  Parts<HD> ps(own_lds, W, rows);
+  Parts<HD> ps(lds, W, rows);
   ps.put(w, wave.run, b.n);
   __syncthreads();
-  if (runs == 1) {
-    const int n = shared_parts(own.skip, parts);
-    for (int i = threadIdx.x; i < b.n * (HD / 4); i += blockDim.x)
-      join_column<HD, T, W>(a, sp, env, b.head0 + i / (HD / 4), 4 * (i % (HD / 4)), n, 0, 0, &ps, i / (HD / 4));
-    return;
-  }
   const size_t to = (parts + run) * sp.columns + (size_t)env * a.n_heads + b.head0;
   for (int i = threadIdx.x; i < b.n * (HD / 4); i += blockDim.x) {
     const int h = i / (HD / 4), f = 4 * (i % (HD / 4));
@@ -312,80 +264,114 @@ __global__ __launch_bounds__(64 * W) void attn_own_kernel(SharedArgs args, PartS
   }
 }
 
-// One wave per head (HD 64: a quarter of it; 256: all).
+template <int HD, CacheType T, int QT, int NW>
+__global__ __launch_bounds__(64 * NW, HD == 256 || (HD == 128 && QT == 2) ? 1 : 2) void attn_parts_kernel(SharedArgs args, PartSpace sp, int shared_blocks,
+                                                                                                         int parts, int runs, int rows) {
+  extern __shared__ __align__(16) char lds[];
+  if ((int)blockIdx.x < shared_blocks) shared_part<HD, T, NW>(args, sp, parts, blockIdx.x, lds);
+  else own_part<HD, T, QT, NW>(args, sp, parts, runs, rows, blockIdx.x - shared_blocks, reinterpret_cast<float*>(lds));
+}
+
+// One workgroup per head of an environment: each thread first takes a part's maximum and sum, then every HD / 4 threads add a share
+// of the parts, four features each.
+constexpr int kMostParts = 128, kSumThreads = 256;
 template <int HD, CacheType T>
-__global__ __launch_bounds__(64) void attn_parts_kernel(SharedArgs args, PartSpace sp, int parts, int runs) {
+__global__ __launch_bounds__(kSumThreads) void attn_sum_kernel(SharedArgs args, PartSpace sp, int parts, int runs) {
+  constexpr int CH = HD / 4, PG = kSumThreads / CH, NW = kSumThreads / kWave;
+  __shared__ float weight[kMostParts], top[NW], total[NW];
+  __shared__ __align__(16) f32x4 sums[PG][CH];
   const PagedAttnArgs& a = args.a;
-  const int env = blockIdx.y, head = blockIdx.x;
+  const int env = blockIdx.y, head = blockIdx.x, tid = threadIdx.x;
   const Own own = own_of<T>(args, env);
   if (own.zeros || own.bad) return fill_rows<HD, T>(a, env, head, 1, own.zeros);
-  const int m = own.steps == 0 ? 0 : (own.steps + run_of(own.steps, runs) - 1) / run_of(own.steps, runs);
-  if (4 * threadIdx.x < HD) join_column<HD, T, 0>(a, sp, env, head, 4 * threadIdx.x, shared_parts(own.skip, parts), parts, m, nullptr, 0);
+  const int n = shared_parts(own.skip, parts), m = own.steps == 0 ? 0 : (own.steps + run_of(own.steps, runs) - 1) / run_of(own.steps, runs);
+  const size_t at = (size_t)env * a.n_heads + head;
+  auto part = [&](int i) { return (i < n ? i : parts + i - n) * sp.columns + at; };
+  const float2 ml = tid < n + m ? sp.ml[part(tid)] : make_float2(-INFINITY, 0.f);
+  float mx = wave_max(ml.x);
+  if ((tid & 63) == 0) top[tid >> 6] = mx;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < NW; ++i) mx = fmaxf(mx, top[i]);
+  const float c = ml.x == -INFINITY ? 1.f : worth(ml.x, mx);  // a part all of whose scores are -inf adds zeros
+  if (tid < kMostParts) weight[tid] = c;
+  const float sum = wave_sum(ml.y * c);
+  if ((tid & 63) == 0) total[tid >> 6] = sum;
+  __syncthreads();
+  const int f = tid % CH, pg = tid / CH;
+  f32x4 v = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int i = pg; i < n + m; i += PG) {
+    const f32x4 o = *reinterpret_cast<const f32x4*>(sp.o + part(i) * HD + 4 * f);
+    const float w = weight[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = fmaf(o[e], w, v[e]);
+  }
+  sums[pg][f] = v;
+  __syncthreads();
+  if (pg != 0) return;
+  float l = 0.f;
+#pragma unroll
+  for (int i = 0; i < NW; ++i) l += total[i];
+#pragma unroll
+  for (int i = 1; i < PG; ++i) v += sums[i][f];
+  store4<T>(a.o + env * a.ld_o + (size_t)head * HD + 4 * f, v, reciprocal(l));
+  if (a.lse && f == 0) a.lse[at] = log_sum<T>(mx, l);
 }
 
 // ------------------------------------------------------------------ host
+constexpr int kSharedWaves = 4;
+long long shared_items(int n_env, int n_groups, int group) { return (long long)n_env * group / (32 * kSharedWaves) + n_groups; }
+
+// Workgroups of both kinds are to run at once, two to a CU: what the environments' own pages leave of 512 goes to the shared ones.
 Plan plan(int n_env, int n_groups, int n_heads, int n_kv_heads, int head_dim, int max_pages) {
   const int group = n_heads / n_kv_heads;
-  Plan p = {false, 2, 1, 1};
-  if (n_groups == 0 || max_pages == 0 || n_env < 2 * n_groups) return p;
-  p.share = true;
-  const long long columns = (long long)n_env * group / n_groups;  // of a group and key head, in the mean
-  p.waves = columns > 128 && head_dim < 256 ? 8 : columns > 64 ? 4 : 2;
-  const long long items = ((long long)n_env * group / (32 * p.waves) + n_groups) * n_kv_heads;
-  p.parts = (int)std::max(1ll, std::min({(512 + items - 1) / items, (max_pages + 7ll) / 8, 64ll}));
-  if (items * p.parts * 64 * p.waves >= 1ll << 32) return {false, 2, 1, 1};  // more threads than a launch takes
+  const Plan none = {false, 1, 1};
+  if (n_groups == 0 || max_pages == 0 || n_env < 2 * n_groups) return none;
   const int tiles = query_tiles(group, head_dim);
   const long long pieces = (long long)n_env * (tiles == 1 ? head_blocks<1>(group) : head_blocks<2>(group)) * n_kv_heads;
-  p.own = (int)std::max(1ll, std::min({(256 + pieces - 1) / pieces, (max_pages + 31ll) / 32, 32ll}));
-  return p;
+  const long long own = std::max(1ll, std::min({256 / pieces, (max_pages + 31ll) / 32, 32ll}));
+  const long long items = shared_items(n_env, n_groups, group) * n_kv_heads, left = 512 - std::min(pieces * own, 256ll);
+  const long long parts = std::max(1ll, std::min({left / items, (max_pages + 7ll) / 8, 64ll}));
+  // more threads than a launch takes: not shared
+  return (items * parts + pieces * own) * 64 * kSharedWaves < 1ll << 32 ? Plan{true, (int)parts, (int)own} : none;
 }
 
-template <int HD, CacheType T, int NW>
-hipError_t launch_shared(const SharedArgs& s, const PartSpace& sp, const Plan& p, hipStream_t stream) {
-  static LdsLimit limit;
-  const auto kernel = attn_shared_kernel<HD, T, NW>;
-  constexpr int kLds = 4 * tiles::kTileBytes<HD>;
-  const hipError_t e = limit.allow((const void*)kernel, kLds);
-  if (e != hipSuccess) return e;
-  const int group = s.a.n_heads / s.a.n_kv_heads;
-  const long long items = (long long)s.a.n_env * group / (32 * NW) + s.n_groups;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)(items * s.a.n_kv_heads * p.parts)), dim3(64 * NW), kLds, stream, s, sp, p.parts);
-  return hipGetLastError();
-}
 template <int HD, CacheType T, int QT>
-hipError_t launch_own(const SharedArgs& s, const PartSpace& sp, const Plan& p, hipStream_t stream) {
-  constexpr int W = 4;
+hipError_t launch_parts(const SharedArgs& s, const PartSpace& sp, const Plan& p, hipStream_t stream) {
+  constexpr int NW = kSharedWaves;
   static LdsLimit limit;
-  const auto kernel = attn_own_kernel<HD, T, QT, W>;
-  hipError_t e = limit.allow((const void*)kernel, Parts<HD>::bytes(W, 16 * QT));
+  const auto kernel = attn_parts_kernel<HD, T, QT, NW>;
+  const int group = s.a.n_heads / s.a.n_kv_heads, rows = query_rows(group, QT);
+  const size_t shared = 4 * tiles::kTileBytes<HD>, most = std::max(shared, Parts<HD>::bytes(NW, 16 * QT));
+  const hipError_t e = limit.allow((const void*)kernel, most);
   if (e != hipSuccess) return e;
-  const int group = s.a.n_heads / s.a.n_kv_heads, blocks = head_blocks<QT>(group) * s.a.n_kv_heads, rows = query_rows(group, QT);
-  hipLaunchKernelGGL(kernel, dim3(blocks * p.own, s.a.n_env), dim3(64 * W), Parts<HD>::bytes(W, rows), stream, s, sp, p.parts, p.own, rows);
-  e = hipGetLastError();
-  if (e != hipSuccess || p.own == 1) return e;
-  hipLaunchKernelGGL((attn_parts_kernel<HD, T>), dim3(s.a.n_heads, s.a.n_env), dim3(64), 0, stream, s, sp, p.parts, p.own);
+  const long long blocks = shared_items(s.a.n_env, s.n_groups, group) * s.a.n_kv_heads * p.parts;
+  const long long pieces = (long long)s.a.n_env * head_blocks<QT>(group) * s.a.n_kv_heads * p.own;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(blocks + pieces)), dim3(64 * NW), std::max(shared, Parts<HD>::bytes(NW, rows)), stream, s, sp,
+                     (int)blocks, p.parts, p.own, rows);
   return hipGetLastError();
 }
-int all_parts(const Plan& p) { return p.parts + (p.own > 1 ? p.own : 0); }
 
-template <int HD, CacheType T>
+template <int HD, CacheType T, int QT>
 hipError_t launch_both(const SharedArgs& s, const Plan& p, hipStream_t stream) {
-  const PartSpace sp = part_space(s.a.ws, s.a, all_parts(p));
-  hipError_t e = hipErrorInvalidValue;
-  if (p.waves == 2) e = launch_shared<HD, T, 2>(s, sp, p, stream);
-  if (p.waves == 4) e = launch_shared<HD, T, 4>(s, sp, p, stream);
-  if constexpr (HD < 256)
-    if (p.waves == 8) e = launch_shared<HD, T, 8>(s, sp, p, stream);
+  const PartSpace sp = part_space(s.a.ws, s.a, p.all());
+  const hipError_t e = launch_parts<HD, T, QT>(s, sp, p, stream);
   if (e != hipSuccess) return e;
+  hipLaunchKernelGGL((attn_sum_kernel<HD, T>), dim3(s.a.n_heads, s.a.n_env), dim3(kSumThreads), 0, stream, s, sp, p.parts, p.own);
+  return hipGetLastError();
+}
+template <int HD, CacheType T>
+hipError_t launch_group(const SharedArgs& s, const Plan& p, hipStream_t stream) {
   if constexpr (HD < 256)
-    if (query_tiles(s.a.n_heads / s.a.n_kv_heads, HD) == 2) return launch_own<HD, T, 2>(s, sp, p, stream);
-  return launch_own<HD, T, 1>(s, sp, p, stream);
+    if (query_tiles(s.a.n_heads / s.a.n_kv_heads, HD) == 2) return launch_both<HD, T, 2>(s, p, stream);
+  return launch_both<HD, T, 1>(s, p, stream);
 }
 template <CacheType T>
 hipError_t launch_dims(const SharedArgs& s, const Plan& p, hipStream_t stream) {
-  if (s.a.head_dim == 64) return launch_both<64, T>(s, p, stream);
-  if (s.a.head_dim == 128) return launch_both<128, T>(s, p, stream);
-  if (s.a.head_dim == 256) return launch_both<256, T>(s, p, stream);
+  if (s.a.head_dim == 64) return launch_group<64, T>(s, p, stream);
+  if (s.a.head_dim == 128) return launch_group<128, T>(s, p, stream);
+  if (s.a.head_dim == 256) return launch_group<256, T>(s, p, stream);
   return hipErrorInvalidValue;
 }
 
@@ -395,7 +381,7 @@ size_t shared_attn_bytes(int n_env, int n_groups, int n_heads, int n_kv_heads, i
   const Plan p = plan(n_env, n_groups, n_heads, n_kv_heads, head_dim, max_pages);
   const size_t plain = paged_attn_bytes(n_env, n_heads, n_kv_heads, head_dim, max_pages);  // also where there are no pages
   if (!p.share) return plain;
-  return std::max(plain, ((size_t)all_parts(p) * n_env * n_heads * (head_dim + 2) * sizeof(float) + 255) / 256 * 256);
+  return std::max(plain, ((size_t)p.all() * n_env * n_heads * (head_dim + 2) * sizeof(float) + 255) / 256 * 256);
 }
 
 hipError_t launch_shared_attn(const SharedArgs& s, hipStream_t stream) {
