@@ -77,15 +77,15 @@ struct Column {
 template <int HD, CacheType T, int NW>
 __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(PromptBwdArgs b, float2* stats) {
   extern __shared__ __align__(16) char lds[];
-  constexpr int M = 32 * NW, KS = HD / 16;
+  constexpr int KS = HD / 16;
   const PromptArgs& a = b.fwd;
-  const int head = blockIdx.x % a.n_heads, item = blockIdx.x / a.n_heads;
+  const int kvh = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads, group = a.n_heads / a.n_kv_heads;
   SeqItem st;
-  if (!find_item<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
+  if (!find_item<NW>(a.row_start, a.n_seq, a.rows, group, item, st)) return;
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int kvh = head / (a.n_heads / a.n_kv_heads);
   const SeqRows k = {a.k.p + st.row0 * a.k.ld + kvh * HD, a.k.ld}, v = {a.v.p + st.row0 * a.v.ld + kvh * HD, a.v.ld};
-  const int q0 = M * st.nth + 32 * wave, qi = q0 + (lane & 31);
+  const int line = NW * st.nth + wave;  // this wave's place in the sequence's line
+  const int q0 = 32 * (line / group), head = kvh * group + line % group, qi = q0 + (lane & 31);
   const bool mine = qi < st.len;
   const int64_t row = st.row0 + (int64_t)min(qi, st.len - 1);
   const ScoreScale sc(a.scale);
@@ -110,66 +110,84 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   Column<HD, T> dq;
   dq.begin();
   const TileLane<HD> at;
-  const int last = (min(M * (st.nth + 1), st.len) - 1) / kTile, own = q0 < st.len ? q0 / kTile : -1;
-  auto tile = [&](int j, int which) { return lds + (2 * (j & 1) + which) * kTileBytes<HD>; };
-  // dS of the 32 keys from 32 t on of tile j, before the scale
-  auto ds_of = [&](int j, int t, bool masked) {
-    f32x16 s = zeros16(), dp;
+  const int last = (min(32 * ((NW * (st.nth + 1) - 1) / group) + 32, st.len) - 1) / kTile, own = q0 < st.len ? q0 / kTile : -1;
+  auto keys = [&](int parity) { return lds + parity * kTileBytes<HD>; };
+  auto values = [&](int parity) { return lds + (2 + parity) * kTileBytes<HD>; };
+  auto copy = [&](int j, int parity) {
+    if (j < 0) return;
+    copy_tile<HD, NW>(keys(parity), k, kTile * j, st.len, wave);
+    copy_tile<HD, NW>(values(parity), v, kTile * j, st.len, wave);
+  };
+  auto arrived = [&] {
+    WAIT_VMCNT(0);
+    __syncthreads();
+  };
+  // dS of the 32 keys from 32 t on of the tile in buffer `parity`, before the scale; keys behind `to` (from the tile's first) none
+  auto ds_of = [&](int parity, int t, int to) {
+    f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
-    for (int r = 0; r < 16; ++r) dp[r] = -d;
+    for (int i = 0; i < KS; ++i) s = mma32<T>(at.rows(keys(parity), 32 * t, i), q[i], s);
 #pragma unroll
-    for (int i = 0; i < KS; ++i) s = mma32<T>(at.rows(tile(j, 0), 32 * t, i), q[i], s);
-#pragma unroll
-    for (int i = 0; i < KS; ++i) dp = mma32<T>(at.rows(tile(j, 1), 32 * t, i), go[i], dp);
+    for (int i = 0; i < KS; ++i) dp = mma32<T>(at.rows(values(parity), 32 * t, i), go[i], dp);
 #pragma unroll
     for (int r = 0; r < 16; ++r) {
-      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.base2, -lse)) * dp[r];
-      if (masked && kTile * j + 32 * t + mma_row(r, h) > qi) s[r] = 0.f;
+      s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.base2, -lse)) * (dp[r] - d);
+      if (to < kTile && 32 * t + mma_row(r, h) > to) s[r] = 0.f;
     }
     return s;
   };
-  copy_tile<HD, NW>(tile(last, 0), k, kTile * last, st.len, wave);
-  copy_tile<HD, NW>(tile(last, 1), v, kTile * last, st.len, wave);
-  WAIT_VMCNT(0);
-  __syncthreads();
-  for (int j = last; j >= 0; --j) {
-    if (j > 0) {
-      copy_tile<HD, NW>(tile(j - 1, 0), k, kTile * (j - 1), st.len, wave);
-      copy_tile<HD, NW>(tile(j - 1, 1), v, kTile * (j - 1), st.len, wave);
-    }
-    if (j < own) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        f32x16 s = ds_of(j, t, false);
-        dq.fit(s);
-        dq.add(at, tile(j, 0), t, s);
-      }
-    } else if (j == own) {
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        f32x16 s = ds_of(j, t, true);
-        dq.fit(s);
-        dq.add(at, tile(j, 0), t, s);
-      }
-      if (__builtin_expect(any_nan(dq.sum), 0)) {  // a masked key may have spoiled the sums: once more without it
-        dq.begin();
-#pragma nounroll
-        for (int t = 0; t < 2; ++t) {
-          f32x16 s = ds_of(j, t, true);
-          dq.fit(s);
-          dq.add_only(tile(j, 0), t, s, 0, qi - kTile * j);
-        }
-      }
-    }
-    WAIT_VMCNT(0);
-    __syncthreads();
+  copy(last, last & 1);
+  arrived();
+  int j = last;
+  for (; j > own; --j) {  // tiles of the workgroup's later queries only
+    copy(j - 1, ~j & 1);
+    arrived();
   }
-  if (own >= 0) store_row<HD, T>(b.dq.p + row * b.dq.ld + head * HD, dq.sum, a.scale / dq.unit, mine);
+  if (own < 0) return;
+  copy(j - 1, ~j & 1);
+  const int to = min(qi - kTile * j, kTile - 1);
+#pragma nounroll
+  for (int t = 0; t < 2; ++t) {
+    f32x16 s = ds_of(j & 1, t, to);
+    dq.fit(s);
+    dq.add(at, keys(j & 1), t, s);
+  }
+  if (__builtin_expect(any_nan(dq.sum), 0)) {  // a masked key may have spoiled the sums: once more without it
+    dq.begin();
+#pragma nounroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 s = ds_of(j & 1, t, to);
+      dq.fit(s);
+      dq.add_only(keys(j & 1), t, s, 0, to);
+    }
+  }
+  arrived();
+  auto tile = [&](int j, int parity) {
+    copy(j - 1, 1 - parity);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      f32x16 s = ds_of(parity, t, kTile);
+      dq.fit(s);
+      dq.add(at, keys(parity), t, s);
+    }
+    arrived();
+  };
+  if (--j >= 0 && j % 2 == 0) {
+    tile(j, 0);
+    --j;
+  }
+  for (; j >= 0; j -= 2) {
+    tile(j, 1);
+    tile(j - 1, 0);
+  }
+  constexpr int kShare = 4 * kTileBytes<HD> / NW;
+  store_rows<HD, T, kShare>(lds + wave * kShare, b.dq.p + (st.row0 + (int64_t)q0) * b.dq.ld + head * HD, b.dq.ld, min(st.len - q0, 32), dq.sum,
+                            a.scale / dq.unit);
 }
 
 // ------------------------------------------------------------------ keys
 template <int HD, CacheType T, int NW>
-__global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats) {
+__global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats) {
   extern __shared__ __align__(16) char lds[];
   constexpr int M = 32 * NW, KS = HD / 16;
   const PromptArgs& a = b.fwd;
@@ -178,7 +196,6 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
   if (!find_item<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int k0 = M * st.nth + 32 * wave, kj = k0 + (lane & 31);
-  const bool mine = kj < st.len;
   const int64_t row = st.row0 + (int64_t)min(kj, st.len - 1);
   const ScoreScale sc(a.scale);
   uint4 k[KS], v[KS];
@@ -193,7 +210,7 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
   const int last_own = (min(M * (st.nth + 1), st.len) - 1) / kTile;                // of the workgroup's last key
   const int own = k0 < st.len ? k0 / kTile : end;                                   // of this wave's keys: the one with masked pairs
   auto tile = [&](int n, int which) { return lds + (2 * (n & 1) + which) * kTileBytes<HD>; };
-  auto stat = [&](int n) { return reinterpret_cast<float2*>(lds + 4 * kTileBytes<HD>) + (n & 1) * kTile; };
+  auto stat = [&](int n) { return reinterpret_cast<float*>(lds + 4 * kTileBytes<HD>) + (n & 1) * 2 * kTile; };  // log-sum-exps, then D
   // tile j of head `head` into buffer n; waits for nothing
   auto copy = [&](int n, int head, int j) {
     const SeqRows q = {a.q.p + st.row0 * a.q.ld + head * HD, a.q.ld};
@@ -202,28 +219,29 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
     copy_tile<HD, NW>(tile(n, 1), go, kTile * j, st.len, wave);
     if (wave == 0) {  // rows behind the last have weights of 0
       const int i = kTile * j + lane;
-      stat(n)[lane] = i < st.len ? stats[(int64_t)head * a.rows + st.row0 + i] : make_float2(INFINITY, 0.f);
+      const float2 x = i < st.len ? stats[(int64_t)head * a.rows + st.row0 + i] : make_float2(INFINITY, 0.f);
+      stat(n)[lane] = x.x;
+      stat(n)[kTile + lane] = x.y;
     }
   };
   // p = weights (times 2^15 in half precision) and ds of the 32 queries from 32 t on of tile j in buffer n
   auto weights = [&](int n, int j, int t, bool masked, f32x16& p, f32x16& ds) {
-    p = zeros16();
-    float lse[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      const float2 x = stat(n)[32 * t + mma_row(r, h)];
-      lse[r] = x.x - kWeightExp<T>;
-      ds[r] = -x.y;
-    }
+    p = ds = zeros16();
 #pragma unroll
     for (int i = 0; i < KS; ++i) p = mma32<T>(at.rows(tile(n, 0), 32 * t, i), k[i], p);
 #pragma unroll
     for (int i = 0; i < KS; ++i) ds = mma32<T>(at.rows(tile(n, 1), 32 * t, i), v[i], ds);
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], sc.base2, -lse[r]));
-      ds[r] *= p[r];
-      if (masked && kTile * j + 32 * t + mma_row(r, h) < kj) p[r] = ds[r] = 0.f;
+    for (int i = 0; i < 4; ++i) {
+      const f32x4 lse = *reinterpret_cast<const f32x4*>(stat(n) + 32 * t + mma_row(4 * i, h));
+      const f32x4 d = *reinterpret_cast<const f32x4*>(stat(n) + kTile + 32 * t + mma_row(4 * i, h));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int r = 4 * i + e;
+        p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], sc.base2, kWeightExp<T> - lse[e]));
+        ds[r] = p[r] * (ds[r] - d[e]);
+        if (masked && kTile * j + 32 * t + mma_row(r, h) < kj) p[r] = ds[r] = 0.f;
+      }
     }
   };
   // All heads' tiles j0 .. j1 - 1 in turn.
@@ -252,7 +270,7 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
   dv.begin();
   over(first, last_own + 1, [&](int n, int j) {
     if (j != own) return;
-#pragma unroll
+#pragma nounroll
     for (int t = 0; t < 2; ++t) {
       f32x16 p, ds;
       weights(n, j, t, true, p, ds);
@@ -281,7 +299,7 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
   }
   over(first + 1, end, [&](int n, int j) {
     if (j <= own) return;
-#pragma unroll
+#pragma nounroll
     for (int t = 0; t < 2; ++t) {
       f32x16 p, ds;
       weights(n, j, t, false, p, ds);
@@ -292,8 +310,11 @@ __global__ __launch_bounds__(64 * NW, HD == 64 ? 2 : 1) void prompt_dkv_kernel(P
   });
   if (own == end) return;
   constexpr float kUnit = T == kBf16 ? 1.f : 0x1p-15f;
-  store_row<HD, T>(b.dk.p + row * b.dk.ld + kvh * HD, dk.sum, a.scale * kUnit / dk.unit, mine);
-  store_row<HD, T>(b.dv.p + row * b.dv.ld + kvh * HD, dv.sum, kUnit, mine);
+  constexpr int kShare = 4 * kTileBytes<HD> / NW;
+  const int64_t first_row = st.row0 + (int64_t)k0;
+  const int n = min(st.len - k0, 32);
+  store_rows<HD, T, kShare>(lds + wave * kShare, b.dk.p + first_row * b.dk.ld + kvh * HD, b.dk.ld, n, dk.sum, a.scale * kUnit / dk.unit);
+  store_rows<HD, T, kShare>(lds + wave * kShare, b.dv.p + first_row * b.dv.ld + kvh * HD, b.dv.ld, n, dv.sum, kUnit);
 }
 
 template <int HD, CacheType T>
@@ -306,8 +327,9 @@ hipError_t launch(const PromptBwdArgs& b, hipStream_t s) {
   if (e == hipSuccess) e = dkv_limit.allow((const void*)dkv, kDkv);
   if (e != hipSuccess) return e;
   const long long items = seq_items<NW>(b.fwd.rows, b.fwd.n_seq, 1);
+  const long long lines = seq_items<NW>(b.fwd.rows, b.fwd.n_seq, b.fwd.n_heads / b.fwd.n_kv_heads);
   float2* stats = static_cast<float2*>(b.ws);
-  hipLaunchKernelGGL(dq, dim3((unsigned)(items * b.fwd.n_heads)), dim3(64 * NW), kDq, s, b, stats);
+  hipLaunchKernelGGL(dq, dim3((unsigned)(lines * b.fwd.n_kv_heads)), dim3(64 * NW), kDq, s, b, stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(dkv, dim3((unsigned)(items * b.fwd.n_kv_heads)), dim3(64 * NW), kDkv, s, b, stats);
   return hipGetLastError();
