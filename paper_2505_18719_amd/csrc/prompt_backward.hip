@@ -186,16 +186,24 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
 }
 
 // ------------------------------------------------------------------ keys
+// Where one workgroup per 128 keys would leave the GPU empty, each has `parts`, which take turns at the queries and leave fp32 sums.
+struct KeyParts {
+  int parts;
+  float* sums;  // [parts][2][rows][n_kv_heads][head_dim], unused with one part
+};
+
 template <int HD, CacheType T, int NW>
-__global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats) {
+__global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats, KeyParts kp) {
   extern __shared__ __align__(16) char lds[];
   constexpr int M = 32 * NW, KS = HD / 16;
   const PromptArgs& a = b.fwd;
-  const int kvh = blockIdx.x % a.n_kv_heads, item = blockIdx.x / a.n_kv_heads, group = a.n_heads / a.n_kv_heads;
+  const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads, part = rest % kp.parts, item = rest / kp.parts;
+  const int group = a.n_heads / a.n_kv_heads;
   SeqItem st;
   if (!find_item<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int k0 = M * st.nth + 32 * wave, kj = k0 + (lane & 31);
+  const int nth = (st.len + M - 1) / M - 1 - st.nth;  // the first keys have the most queries
+  const int k0 = M * nth + 32 * wave, kj = k0 + (lane & 31);
   const int64_t row = st.row0 + (int64_t)min(kj, st.len - 1);
   const ScoreScale sc(a.scale);
   uint4 k[KS], v[KS];
@@ -206,26 +214,33 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   }
   Column<HD, T> dk, dv;
   const TileLane<HD> at;
-  const int first = M * st.nth / kTile, end = (st.len + kTile - 1) / kTile;        // tiles of queries
-  const int last_own = (min(M * (st.nth + 1), st.len) - 1) / kTile;                // of the workgroup's last key
-  const int own = k0 < st.len ? k0 / kTile : end;                                   // of this wave's keys: the one with masked pairs
+  // Tiles of queries: those with the workgroup's keys' own, of which one has pairs of this wave's that are masked, and those behind.
+  const int first = M * nth / kTile, behind = (min(M * (nth + 1), st.len) - 1) / kTile + 1, end = (st.len + kTile - 1) / kTile;
+  const int own = k0 < st.len ? k0 / kTile : end;
   auto tile = [&](int n, int which) { return lds + (2 * (n & 1) + which) * kTileBytes<HD>; };
   auto stat = [&](int n) { return reinterpret_cast<float*>(lds + 4 * kTileBytes<HD>) + (n & 1) * 2 * kTile; };  // log-sum-exps, then D
-  // tile j of head `head` into buffer n; waits for nothing
+  // Tile j of head `head` into buffer n.  Its rows' statistics pass through a register of the first wave, which puts them there after
+  // the tile before has been used: rows behind the last have weights of 0.
+  float2 x = make_float2(INFINITY, 0.f);
   auto copy = [&](int n, int head, int j) {
     const SeqRows q = {a.q.p + st.row0 * a.q.ld + head * HD, a.q.ld};
     const SeqRows go = {b.dout.p + st.row0 * b.dout.ld + head * HD, b.dout.ld};
     copy_tile<HD, NW>(tile(n, 0), q, kTile * j, st.len, wave);
     copy_tile<HD, NW>(tile(n, 1), go, kTile * j, st.len, wave);
-    if (wave == 0) {  // rows behind the last have weights of 0
-      const int i = kTile * j + lane;
-      const float2 x = i < st.len ? stats[(int64_t)head * a.rows + st.row0 + i] : make_float2(INFINITY, 0.f);
+    const int i = kTile * j + lane;
+    if (wave == 0) x = i < st.len ? stats[(int64_t)head * a.rows + st.row0 + i] : make_float2(INFINITY, 0.f);
+  };
+  auto arrived = [&](int n) {
+    if (wave == 0) {
       stat(n)[lane] = x.x;
       stat(n)[kTile + lane] = x.y;
     }
+    WAIT_VMCNT(0);
+    __syncthreads();
   };
-  // p = weights (times 2^15 in half precision) and ds of the 32 queries from 32 t on of tile j in buffer n
-  auto weights = [&](int n, int j, int t, bool masked, f32x16& p, f32x16& ds) {
+  // Weights p (times 2^15 in half precision) and ds of the 32 queries from 32 t on of the tile in buffer n; those before `from` (from
+  // the tile's first) do not see the lane's key.
+  auto weights = [&](int n, int t, int from, bool masked, f32x16& p, f32x16& ds) {
     p = ds = zeros16();
 #pragma unroll
     for (int i = 0; i < KS; ++i) p = mma32<T>(at.rows(tile(n, 0), 32 * t, i), k[i], p);
@@ -240,19 +255,17 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
         const int r = 4 * i + e;
         p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], sc.base2, kWeightExp<T> - lse[e]));
         ds[r] = p[r] * (ds[r] - d[e]);
-        if (masked && kTile * j + 32 * t + mma_row(r, h) < kj) p[r] = ds[r] = 0.f;
+        if (masked && 32 * t + mma_row(r, h) < from) p[r] = ds[r] = 0.f;
       }
     }
   };
-  // All heads' tiles j0 .. j1 - 1 in turn.
+  // All heads' tiles j0 .. j1 - 1 in turn, or this part's share of them.
   auto over = [&](int j0, int j1, auto&& take) {
-    if (j0 >= j1) return;
-    const int n = group * (j1 - j0);
-    int head = kvh * group, j = j0;
-    __syncthreads();  // what the buffers held has been used
+    const int all = group * (j1 - j0), s0 = (int)((long long)all * part / kp.parts), n = (int)((long long)all * (part + 1) / kp.parts) - s0;
+    if (n <= 0) return;
+    int head = kvh * group + s0 / (j1 - j0), j = j0 + s0 % (j1 - j0);
     copy(0, head, j);
-    WAIT_VMCNT(0);
-    __syncthreads();
+    arrived(0);
     for (int i = 0; i < n; ++i) {
       const int now = j;
       if (++j == j1) {
@@ -260,49 +273,45 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
         ++head;
       }
       if (i + 1 < n) copy(i + 1, head, j);
-      take(i, now);
-      WAIT_VMCNT(0);
-      __syncthreads();
+      if (now >= own) take(i, now);
+      arrived(i + 1);
     }
   };
-  // First the tiles part of whose pairs are masked, of all heads; then the whole ones.
   dk.begin();
   dv.begin();
-  over(first, last_own + 1, [&](int n, int j) {
-    if (j != own) return;
+  over(first, behind, [&](int n, int j) {
 #pragma nounroll
     for (int t = 0; t < 2; ++t) {
       f32x16 p, ds;
-      weights(n, j, t, true, p, ds);
+      weights(n, t, kj - kTile * j, true, p, ds);
       dv.add(at, tile(n, 1), t, p);
       dk.fit(ds);
       dk.add(at, tile(n, 0), t, ds);
     }
   });
   const bool spoiled = any_nan(dk.sum) || any_nan(dv.sum);
-  if (__builtin_expect(__builtin_amdgcn_readfirstlane(__syncthreads_or(spoiled)), 0)) {  // masked queries may have spoiled the sums: once more without them
-    if (spoiled) {
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(__syncthreads_or(spoiled)), 0)) {  // masked queries may have spoiled the sums: once
+    if (spoiled) {                                                                        // more without them
       dk.begin();
       dv.begin();
     }
-    over(first, last_own + 1, [&](int n, int j) {
-      if (j != own || !spoiled) return;
+    over(first, behind, [&](int n, int j) {
+      if (!spoiled) return;
 #pragma nounroll
       for (int t = 0; t < 2; ++t) {
         f32x16 p, ds;
-        weights(n, j, t, true, p, ds);
+        weights(n, t, kj - kTile * j, true, p, ds);
         dv.add_only(tile(n, 1), t, p, kj - kTile * j, kTile);
         dk.fit(ds);
         dk.add_only(tile(n, 0), t, ds, kj - kTile * j, kTile);
       }
     });
   }
-  over(first + 1, end, [&](int n, int j) {
-    if (j <= own) return;
+  over(behind, end, [&](int n, int j) {
 #pragma nounroll
     for (int t = 0; t < 2; ++t) {
       f32x16 p, ds;
-      weights(n, j, t, false, p, ds);
+      weights(n, t, 0, false, p, ds);
       dv.add(at, tile(n, 1), t, p);
       dk.fit(ds);
       dk.add(at, tile(n, 0), t, ds);
@@ -310,28 +319,97 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   });
   if (own == end) return;
   constexpr float kUnit = T == kBf16 ? 1.f : 0x1p-15f;
-  constexpr int kShare = 4 * kTileBytes<HD> / NW;
   const int64_t first_row = st.row0 + (int64_t)k0;
   const int n = min(st.len - k0, 32);
-  store_rows<HD, T, kShare>(lds + wave * kShare, b.dk.p + first_row * b.dk.ld + kvh * HD, b.dk.ld, n, dk.sum, a.scale * kUnit / dk.unit);
-  store_rows<HD, T, kShare>(lds + wave * kShare, b.dv.p + first_row * b.dv.ld + kvh * HD, b.dv.ld, n, dv.sum, kUnit);
+  const float mul = a.scale * kUnit / dk.unit;
+  if (kp.parts == 1) {
+    constexpr int kShare = 4 * kTileBytes<HD> / NW;
+    store_rows<HD, T, kShare>(lds + wave * kShare, b.dk.p + first_row * b.dk.ld + kvh * HD, b.dk.ld, n, dk.sum, mul);
+    store_rows<HD, T, kShare>(lds + wave * kShare, b.dv.p + first_row * b.dv.ld + kvh * HD, b.dv.ld, n, dv.sum, kUnit);
+    return;
+  }
+  if ((lane & 31) >= n) return;
+  const int64_t width = (int64_t)a.n_kv_heads * HD;
+  float* to = kp.sums + 2 * part * a.rows * width + row * width + kvh * HD + 4 * h;
+#pragma unroll
+  for (int mb = 0; mb < HD / 32; ++mb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      f32x4 u, w;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        u[e] = dk.sum[mb][4 * i + e] * mul;
+        w[e] = dv.sum[mb][4 * i + e] * kUnit;
+      }
+      *reinterpret_cast<f32x4*>(to + 32 * mb + 8 * i) = u;
+      *reinterpret_cast<f32x4*>(to + a.rows * width + 32 * mb + 8 * i) = w;
+    }
 }
+
+// Adds the parts' sums in order, four features a thread, of the rows of sequences.
+constexpr int kSumThreads = 256;
+template <CacheType T>
+__global__ __launch_bounds__(kSumThreads) void prompt_sum_kernel(PromptBwdArgs b, KeyParts kp, int width) {
+  const PromptArgs& a = b.fwd;
+  const int64_t i = (int64_t)blockIdx.x * kSumThreads + threadIdx.x, row = i / (width / 4);
+  const int f = 4 * (int)(i % (width / 4));
+  if (row >= a.rows) return;
+  // the last sequence that begins at or before the row
+  int lo = 0, n = a.n_seq;
+  while (n > 1) {
+    const int half = n / 2;
+    if (a.row_start[lo + half] <= row) {
+      lo += half;
+      n -= half;
+    } else {
+      n = half;
+    }
+  }
+  const int start = a.row_start[lo], end = a.row_start[lo + 1];
+  if (start < 0 || start > row || end <= row || end > a.rows) return;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    f32x4 s = {0.f, 0.f, 0.f, 0.f};
+    for (int p = 0; p < kp.parts; ++p) s += *reinterpret_cast<const f32x4*>(kp.sums + ((2 * p + w) * (int64_t)a.rows + row) * width + f);
+    const HeadRows& to = w == 0 ? b.dk : b.dv;
+    *reinterpret_cast<uint2*>(to.p + row * to.ld + f) = make_uint2(pack2<T>(s[0], s[1]), pack2<T>(s[2], s[3]));
+  }
+}
+
+// ------------------------------------------------------------------ host
+constexpr int kWaves = 4;
+
+// Parts of each 128 keys' queries: enough to fill the GPU twice over, as the first keys of a sequence have many times the work of the
+// last ones.
+int key_parts(int rows, int n_seq, int n_heads, int n_kv_heads) {
+  const long long groups = seq_items<kWaves>(rows, n_seq, 1) * n_kv_heads;
+  const long long steps = ((long long)rows / n_seq / kTile + 1) * (n_heads / n_kv_heads);  // of a workgroup, about
+  return (int)std::max(1ll, std::min({1024 / groups, steps / 8, 16ll}));
+}
+size_t stat_bytes(int rows, int n_heads) { return ((size_t)rows * n_heads * sizeof(float2) + 255) / 256 * 256; }
 
 template <int HD, CacheType T>
 hipError_t launch(const PromptBwdArgs& b, hipStream_t s) {
-  constexpr int NW = 4, kDq = 4 * kTileBytes<HD>, kDkv = kDq + 2 * kTile * (int)sizeof(float2);
+  constexpr int NW = kWaves, kDq = 4 * kTileBytes<HD>, kDkv = kDq + 4 * kTile * (int)sizeof(float);
   static LdsLimit dq_limit, dkv_limit;
   const auto dq = prompt_dq_kernel<HD, T, NW>;
   const auto dkv = prompt_dkv_kernel<HD, T, NW>;
   hipError_t e = dq_limit.allow((const void*)dq, kDq);
   if (e == hipSuccess) e = dkv_limit.allow((const void*)dkv, kDkv);
   if (e != hipSuccess) return e;
-  const long long items = seq_items<NW>(b.fwd.rows, b.fwd.n_seq, 1);
-  const long long lines = seq_items<NW>(b.fwd.rows, b.fwd.n_seq, b.fwd.n_heads / b.fwd.n_kv_heads);
+  const PromptArgs& a = b.fwd;
+  const long long items = seq_items<NW>(a.rows, a.n_seq, 1);
+  const long long lines = seq_items<NW>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads);
   float2* stats = static_cast<float2*>(b.ws);
-  hipLaunchKernelGGL(dq, dim3((unsigned)(lines * b.fwd.n_kv_heads)), dim3(64 * NW), kDq, s, b, stats);
+  const KeyParts kp = {key_parts(a.rows, a.n_seq, a.n_heads, a.n_kv_heads),
+                       reinterpret_cast<float*>(static_cast<char*>(b.ws) + stat_bytes(a.rows, a.n_heads))};
+  hipLaunchKernelGGL(dq, dim3((unsigned)(lines * a.n_kv_heads)), dim3(64 * NW), kDq, s, b, stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(dkv, dim3((unsigned)(items * b.fwd.n_kv_heads)), dim3(64 * NW), kDkv, s, b, stats);
+  hipLaunchKernelGGL(dkv, dim3((unsigned)(items * a.n_kv_heads * kp.parts)), dim3(64 * NW), kDkv, s, b, stats, kp);
+  if ((e = hipGetLastError()) != hipSuccess || kp.parts == 1) return e;
+  const int width = a.n_kv_heads * HD;
+  const long long threads = (long long)a.rows * (width / 4);
+  hipLaunchKernelGGL(prompt_sum_kernel<T>, dim3((unsigned)((threads + kSumThreads - 1) / kSumThreads)), dim3(kSumThreads), 0, s, b, kp, width);
   return hipGetLastError();
 }
 
@@ -346,7 +424,9 @@ hipError_t launch_type(const PromptBwdArgs& b, hipStream_t s) {
 }  // namespace
 
 size_t prompt_bwd_bytes(int rows, int n_seq, int n_heads, int n_kv_heads, int head_dim) {
-  return ((size_t)rows * n_heads * sizeof(float2) + 255) / 256 * 256;
+  if (rows == 0 || n_seq == 0) return 0;
+  const int parts = key_parts(rows, n_seq, n_heads, n_kv_heads);
+  return stat_bytes(rows, n_heads) + (parts == 1 ? 0 : (size_t)parts * 2 * rows * n_kv_heads * head_dim * sizeof(float));
 }
 
 hipError_t launch_prompt_attn_bwd(const PromptBwdArgs& b, hipStream_t s) {
