@@ -200,7 +200,7 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads, part = rest % kp.parts, item = rest / kp.parts;
   const int group = a.n_heads / a.n_kv_heads;
   SeqItem st;
-  if (!find_item<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
+  if (!find_sorted<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nth = (st.len + M - 1) / M - 1 - st.nth;  // the first keys have the most queries
   const int k0 = M * nth + 32 * wave, kj = k0 + (lane & 31);
