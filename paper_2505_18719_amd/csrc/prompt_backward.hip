@@ -56,15 +56,27 @@ struct Column {
     }
   }
   // sum += x^T w over the 32 rows of a tile from 32 t on, w rounded to the type: a relative 2^-9 (2^-12), of either sign, of each
-  // term at most, beside the output's own rounding
+  // term at most, beside the output's own rounding.  PAIR: w as hi + lo of the type, twice the bits.
+  template <bool PAIR = false>
   __device__ __forceinline__ void add(const TileLane<HD>& at, const char* tile, int t, const f32x16& w) {
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
-      const int r = 8 * b;
-      const uint4 p = make_uint4(pack2<T>(w[r], w[r + 1]), pack2<T>(w[r + 2], w[r + 3]), pack2<T>(w[r + 4], w[r + 5]),
-                                 pack2<T>(w[r + 6], w[r + 7]));
+      uint32_t p[4], rest[4];
 #pragma unroll
-      for (int i = 0; i < HD / 32; ++i) sum[i] = mma32<T>(at.cols(tile, 2 * t + b, i), p, sum[i]);
+      for (int e = 0; e < 4; ++e) {
+        const int r = 8 * b + 2 * e;
+        p[e] = pack2<T>(w[r], w[r + 1]);
+        if constexpr (PAIR) {
+          const float2 hi = unpack2<T>(p[e]);
+          rest[e] = pack2<T>(w[r] - hi.x, w[r + 1] - hi.y);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < HD / 32; ++i) {
+        const uint4 x = at.cols(tile, 2 * t + b, i);
+        sum[i] = mma32<T>(x, make_uint4(p[0], p[1], p[2], p[3]), sum[i]);
+        if constexpr (PAIR) sum[i] = mma32<T>(x, make_uint4(rest[0], rest[1], rest[2], rest[3]), sum[i]);
+      }
     }
   }
   // The same with only the rows from `first` to `last` of the tile.
@@ -106,7 +118,6 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   }
   d = half_sum(d);
   const float lse = lse_base2(a.lse[row * a.n_heads + head]);
-  if (mine && lane < 32) stats[(int64_t)head * a.rows + row] = make_float2(lse, d);
   Column<HD, T> dq;
   dq.begin();
   const TileLane<HD> at;
@@ -122,8 +133,12 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
     WAIT_VMCNT(0);
     __syncthreads();
   };
+  // A row's dS add up to 0 but for what the rounding of its output made of D: the keys' pass gets D with that taken back.  This pass
+  // cannot wait for it, and holds dS in pairs of numbers of the type instead (errors relative to the gradient of bf16 inputs of 279
+  // rows, whose own rounding is 1.66e-3: of dk 2.7e-3 with neither, 2.3e-3 with D; of dq 2.8e-3 with neither, 2.2e-3 with pairs).
+  float excess = 0.f;
   // dS of the 32 keys from 32 t on of the tile in buffer `parity`, before the scale; keys behind `to` (from the tile's first) none
-  auto ds_of = [&](int parity, int t, int to) {
+  auto ds_of = [&](int parity, int t, int to, bool count) {
     f32x16 s = zeros16(), dp = zeros16();
 #pragma unroll
     for (int i = 0; i < KS; ++i) s = mma32<T>(at.rows(keys(parity), 32 * t, i), q[i], s);
@@ -133,6 +148,12 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
     for (int r = 0; r < 16; ++r) {
       s[r] = __builtin_amdgcn_exp2f(fmaf(s[r], sc.base2, -lse)) * (dp[r] - d);
       if (to < kTile && 32 * t + mma_row(r, h) > to) s[r] = 0.f;
+    }
+    if (count) {
+      float sum[2] = {0.f, 0.f};
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sum[r & 1] += s[r];
+      excess += sum[0] + sum[1];
     }
     return s;
   };
@@ -148,15 +169,15 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   const int to = min(qi - kTile * j, kTile - 1);
 #pragma nounroll
   for (int t = 0; t < 2; ++t) {
-    f32x16 s = ds_of(j & 1, t, to);
+    f32x16 s = ds_of(j & 1, t, to, true);
     dq.fit(s);
-    dq.add(at, keys(j & 1), t, s);
+    dq.template add<true>(at, keys(j & 1), t, s);
   }
   if (__builtin_expect(any_nan(dq.sum), 0)) {  // a masked key may have spoiled the sums: once more without it
     dq.begin();
 #pragma nounroll
     for (int t = 0; t < 2; ++t) {
-      f32x16 s = ds_of(j & 1, t, to);
+      f32x16 s = ds_of(j & 1, t, to, false);
       dq.fit(s);
       dq.add_only(keys(j & 1), t, s, 0, to);
     }
@@ -164,11 +185,11 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   arrived();
   auto tile = [&](int j, int parity) {
     copy(j - 1, 1 - parity);
-#pragma unroll
+#pragma nounroll
     for (int t = 0; t < 2; ++t) {
-      f32x16 s = ds_of(parity, t, kTile);
+      f32x16 s = ds_of(parity, t, kTile, true);
       dq.fit(s);
-      dq.add(at, keys(parity), t, s);
+      dq.template add<true>(at, keys(parity), t, s);
     }
     arrived();
   };
@@ -180,6 +201,8 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
     tile(j, 1);
     tile(j - 1, 0);
   }
+  excess = half_sum(excess);
+  if (mine && lane < 32) stats[(int64_t)head * a.rows + row] = make_float2(lse, d + excess);
   constexpr int kShare = 4 * kTileBytes<HD> / NW;
   store_rows<HD, T, kShare>(lds + wave * kShare, b.dq.p + (st.row0 + (int64_t)q0) * b.dq.ld + head * HD, b.dq.ld, min(st.len - q0, 32), dq.sum,
                             a.scale / dq.unit);
@@ -192,10 +215,13 @@ struct KeyParts {
   float* sums;  // [parts][2][rows][n_kv_heads][head_dim], unused with one part
 };
 
-template <int HD, CacheType T, int NW>
+// WHAT: 1 dK, 2 dV, 3 both.  At head_dim 256 the sums of one alone fill half the registers: each has a launch of its own there, and
+// scores are computed once more.
+template <int HD, CacheType T, int NW, int WHAT>
 __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats, KeyParts kp) {
   extern __shared__ __align__(16) char lds[];
   constexpr int M = 32 * NW, KS = HD / 16;
+  constexpr bool DK = WHAT & 1, DV = WHAT & 2;
   const PromptArgs& a = b.fwd;
   const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads, part = rest % kp.parts, item = rest / kp.parts;
   const int group = a.n_heads / a.n_kv_heads;
@@ -244,8 +270,10 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
     p = ds = zeros16();
 #pragma unroll
     for (int i = 0; i < KS; ++i) p = mma32<T>(at.rows(tile(n, 0), 32 * t, i), k[i], p);
+    if constexpr (DK) {
 #pragma unroll
-    for (int i = 0; i < KS; ++i) ds = mma32<T>(at.rows(tile(n, 1), 32 * t, i), v[i], ds);
+      for (int i = 0; i < KS; ++i) ds = mma32<T>(at.rows(tile(n, 1), 32 * t, i), v[i], ds);
+    }
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       const f32x4 lse = *reinterpret_cast<const f32x4*>(stat(n) + 32 * t + mma_row(4 * i, h));
@@ -277,6 +305,13 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
       arrived(i + 1);
     }
   };
+  auto add = [&](int n, int t, const f32x16& p, f32x16& ds) {
+    if constexpr (DV) dv.add(at, tile(n, 1), t, p);
+    if constexpr (DK) {
+      dk.fit(ds);
+      dk.add(at, tile(n, 0), t, ds);
+    }
+  };
   dk.begin();
   dv.begin();
   over(first, behind, [&](int n, int j) {
@@ -284,12 +319,10 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
     for (int t = 0; t < 2; ++t) {
       f32x16 p, ds;
       weights(n, t, kj - kTile * j, true, p, ds);
-      dv.add(at, tile(n, 1), t, p);
-      dk.fit(ds);
-      dk.add(at, tile(n, 0), t, ds);
+      add(n, t, p, ds);
     }
   });
-  const bool spoiled = any_nan(dk.sum) || any_nan(dv.sum);
+  const bool spoiled = (DK && any_nan(dk.sum)) || (DV && any_nan(dv.sum));
   if (__builtin_expect(__builtin_amdgcn_readfirstlane(__syncthreads_or(spoiled)), 0)) {  // masked queries may have spoiled the sums: once
     if (spoiled) {                                                                        // more without them
       dk.begin();
@@ -301,9 +334,11 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
       for (int t = 0; t < 2; ++t) {
         f32x16 p, ds;
         weights(n, t, kj - kTile * j, true, p, ds);
-        dv.add_only(tile(n, 1), t, p, kj - kTile * j, kTile);
-        dk.fit(ds);
-        dk.add_only(tile(n, 0), t, ds, kj - kTile * j, kTile);
+        if constexpr (DV) dv.add_only(tile(n, 1), t, p, kj - kTile * j, kTile);
+        if constexpr (DK) {
+          dk.fit(ds);
+          dk.add_only(tile(n, 0), t, ds, kj - kTile * j, kTile);
+        }
       }
     });
   }
@@ -312,9 +347,7 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
     for (int t = 0; t < 2; ++t) {
       f32x16 p, ds;
       weights(n, t, 0, false, p, ds);
-      dv.add(at, tile(n, 1), t, p);
-      dk.fit(ds);
-      dk.add(at, tile(n, 0), t, ds);
+      add(n, t, p, ds);
     }
   });
   if (own == end) return;
@@ -324,8 +357,8 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   const float mul = a.scale * kUnit / dk.unit;
   if (kp.parts == 1) {
     constexpr int kShare = 4 * kTileBytes<HD> / NW;
-    store_rows<HD, T, kShare>(lds + wave * kShare, b.dk.p + first_row * b.dk.ld + kvh * HD, b.dk.ld, n, dk.sum, mul);
-    store_rows<HD, T, kShare>(lds + wave * kShare, b.dv.p + first_row * b.dv.ld + kvh * HD, b.dv.ld, n, dv.sum, kUnit);
+    if constexpr (DK) store_rows<HD, T, kShare>(lds + wave * kShare, b.dk.p + first_row * b.dk.ld + kvh * HD, b.dk.ld, n, dk.sum, mul);
+    if constexpr (DV) store_rows<HD, T, kShare>(lds + wave * kShare, b.dv.p + first_row * b.dv.ld + kvh * HD, b.dv.ld, n, dv.sum, kUnit);
     return;
   }
   if ((lane & 31) >= n) return;
@@ -341,8 +374,8 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
         u[e] = dk.sum[mb][4 * i + e] * mul;
         w[e] = dv.sum[mb][4 * i + e] * kUnit;
       }
-      *reinterpret_cast<f32x4*>(to + 32 * mb + 8 * i) = u;
-      *reinterpret_cast<f32x4*>(to + a.rows * width + 32 * mb + 8 * i) = w;
+      if constexpr (DK) *reinterpret_cast<f32x4*>(to + 32 * mb + 8 * i) = u;
+      if constexpr (DV) *reinterpret_cast<f32x4*>(to + a.rows * width + 32 * mb + 8 * i) = w;
     }
 }
 
@@ -388,14 +421,23 @@ int key_parts(int rows, int n_seq, int n_heads, int n_kv_heads) {
 }
 size_t stat_bytes(int rows, int n_heads) { return ((size_t)rows * n_heads * sizeof(float2) + 255) / 256 * 256; }
 
+template <int HD, CacheType T, int WHAT>
+hipError_t launch_dkv(const PromptBwdArgs& b, long long groups, const float2* stats, const KeyParts& kp, hipStream_t s) {
+  constexpr int kLds = 4 * kTileBytes<HD> + 4 * kTile * (int)sizeof(float);
+  static LdsLimit limit;
+  const auto kernel = prompt_dkv_kernel<HD, T, kWaves, WHAT>;
+  const hipError_t e = limit.allow((const void*)kernel, kLds);
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * kWaves), kLds, s, b, stats, kp);
+  return hipGetLastError();
+}
+
 template <int HD, CacheType T>
 hipError_t launch(const PromptBwdArgs& b, hipStream_t s) {
-  constexpr int NW = kWaves, kDq = 4 * kTileBytes<HD>, kDkv = kDq + 4 * kTile * (int)sizeof(float);
-  static LdsLimit dq_limit, dkv_limit;
+  constexpr int NW = kWaves, kDq = 4 * kTileBytes<HD>;
+  static LdsLimit limit;
   const auto dq = prompt_dq_kernel<HD, T, NW>;
-  const auto dkv = prompt_dkv_kernel<HD, T, NW>;
-  hipError_t e = dq_limit.allow((const void*)dq, kDq);
-  if (e == hipSuccess) e = dkv_limit.allow((const void*)dkv, kDkv);
+  hipError_t e = limit.allow((const void*)dq, kDq);
   if (e != hipSuccess) return e;
   const PromptArgs& a = b.fwd;
   const long long items = seq_items<NW>(a.rows, a.n_seq, 1);
@@ -405,8 +447,14 @@ hipError_t launch(const PromptBwdArgs& b, hipStream_t s) {
                        reinterpret_cast<float*>(static_cast<char*>(b.ws) + stat_bytes(a.rows, a.n_heads))};
   hipLaunchKernelGGL(dq, dim3((unsigned)(lines * a.n_kv_heads)), dim3(64 * NW), kDq, s, b, stats);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(dkv, dim3((unsigned)(items * a.n_kv_heads * kp.parts)), dim3(64 * NW), kDkv, s, b, stats, kp);
-  if ((e = hipGetLastError()) != hipSuccess || kp.parts == 1) return e;
+  const long long groups = items * a.n_kv_heads * kp.parts;
+  if constexpr (HD == 256) {
+    e = launch_dkv<HD, T, 1>(b, groups, stats, kp, s);
+    if (e == hipSuccess) e = launch_dkv<HD, T, 2>(b, groups, stats, kp, s);
+  } else {
+    e = launch_dkv<HD, T, 3>(b, groups, stats, kp, s);
+  }
+  if (e != hipSuccess || kp.parts == 1) return e;
   const int width = a.n_kv_heads * HD;
   const long long threads = (long long)a.rows * (width / 4);
   hipLaunchKernelGGL(prompt_sum_kernel<T>, dim3((unsigned)((threads + kSumThreads - 1) / kSumThreads)), dim3(kSumThreads), 0, s, b, kp, width);

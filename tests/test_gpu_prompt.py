@@ -276,8 +276,18 @@ def test_rows_far_into_a_large_buffer():
     ss, slse = i32([0, 30, 90]), torch.empty((90, H), device="cuda")
     sout = vla.prompt_attention(*small, ss, 0.2, lse=slse)
     assert torch.equal(sout, out[-90:]) and torch.equal(slse, lse[-90:])
-    for a, b in zip(vla.prompt_attention_backward(*small, sout, slse, do[-90:], ss, 0.2), g):
-        assert torch.equal(a, b[-90:])
+    again = vla.prompt_attention_backward(*small, sout, slse, do[-90:], ss, 0.2)
+    assert torch.equal(again[0], g[0][-90:])
+    # the keys' sums may be split otherwise among as many rows: two results within the same bound of the formulas'
+    c = Case.__new__(Case)
+    c.hd, c.dtype = hd, BF
+    x64 = [f64(t) for t in small]
+    _, _, mag, smax = po.attention(*x64, [0, 30, 90], 0.2)
+    out_err = half_step(f64(sout), BF) + mag * (c.unit_w() + 3 * c.unit_p() * np.maximum(smax, 1.0)[..., None])
+    ref, err = po.backward(*x64, f64(do[-90:]), [0, 30, 90], 0.2, c.unit_w(), 3 * c.unit_p(), (hd + 32) * U32, out_err)
+    for i in (1, 2):
+        for got in (again[i], g[i][-90:]):
+            assert np.all(np.abs(f64(got) - ref[i]) <= half_step(ref[i], BF) * (1 + 2 ** -6) + err[i])
 
 
 def test_single_rows_and_none():
