@@ -69,7 +69,7 @@ def store_case(k, v, slots, n_pages, strided=False):
 def test_store_and_read(hd, dtype, K):
     """Rows anywhere, in runs from any slot on, and outside the pool, of every size the type holds."""
     rng = np.random.default_rng(hd + K)
-    for rows in (1, 2, 17, 100, 333):
+    for rows in (1, 2, 17, 100, 333, 2100):  # the last in workgroups of 64 rows, with 8 heads
         n_pages = rows // PAGE + 9
         order = rng.permutation(n_pages * PAGE)[:rows]
         start = int(rng.integers(0, 40))
