@@ -40,6 +40,7 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
   w.load(a.q.p + row * a.q.ld + head * HD, a.scale);
   const TileLane<HD> at;
   const int last = (min(32 * ((NW * (st.nth + 1) - 1) / group) + 32, st.len) - 1) / kTile;  // tile of the workgroup's last query
+  const int halves = q0 % kTile / 32 + 1;  // of its own tile, those with keys that some query sees
   const int own = q0 < st.len ? q0 / kTile : -1;                                          // of this wave's queries
   // Buffers by the parity of the tile, at places that the loop over pairs of tiles knows beforehand.
   auto keys = [&](int parity) { return lds + parity * kTileBytes<HD>; };
@@ -57,13 +58,13 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
   copy_values(last, last & 1);
   copy_keys(last - 1, ~last & 1);
   arrived();
-  if (own == last) w.scores(at, keys(last & 1), s);
+  if (own == last) w.scores(at, keys(last & 1), s, halves);
   __syncthreads();
   int j = last;
   for (; j > own; --j) {  // tiles of the workgroup's later queries only
     copy_keys(j - 2, j & 1);
     copy_values(j - 1, ~j & 1);
-    if (j - 1 == own) w.scores(at, keys(~j & 1), s);
+    if (j - 1 == own) w.scores(at, keys(~j & 1), s, halves);
     arrived();
   }
   if (own < 0) return;
@@ -74,7 +75,7 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
 #pragma unroll
   for (int t = 0; t < kTile / 32; ++t) next[t] = s[t];
   w.weigh(next);
-  w.add(at, values(j & 1), next);
+  w.add(at, values(j & 1), next, halves);
   if (__builtin_expect(any_nan(w.o), 0)) {  // a masked value may have spoiled the sums: once more without it
     const float l = w.l;
     w.weigh(s);

@@ -166,9 +166,9 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   }
   if (own < 0) return;
   copy(j - 1, ~j & 1);
-  const int to = min(qi - kTile * j, kTile - 1);
+  const int to = min(qi - kTile * j, kTile - 1), halves = q0 % kTile / 32 + 1;  // of the own tile, those with keys that some query sees
 #pragma nounroll
-  for (int t = 0; t < 2; ++t) {
+  for (int t = 0; t < halves; ++t) {
     f32x16 s = ds_of(j & 1, t, to, true);
     dq.fit(s);
     dq.template add<true>(at, keys(j & 1), t, s);
@@ -176,7 +176,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   if (__builtin_expect(any_nan(dq.sum), 0)) {  // a masked key may have spoiled the sums: once more without it
     dq.begin();
 #pragma nounroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < halves; ++t) {
       f32x16 s = ds_of(j & 1, t, to, false);
       dq.fit(s);
       dq.add_only(keys(j & 1), t, s, 0, to);

@@ -265,12 +265,13 @@ struct Queries {
     for (int i = 0; i < MB; ++i) o[i] = zeros16();
   }
 
-  // s = scores of the tile's keys
+  // s = scores of the tile's keys, or of its first `n` times 32
   template <bool PAGES>
-  __device__ __forceinline__ void scores(const TileLane<HD, PAGES>& at, const char* k, Scores& s) {
+  __device__ __forceinline__ void scores(const TileLane<HD, PAGES>& at, const char* k, Scores& s, int n = N) {
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       s[t] = zeros16();
+      if (t >= n) continue;
 #pragma unroll
       for (int i = 0; i < KS; ++i) s[t] = mma32<T>(at.rows(k, 32 * t, i), q[i], s[t]);
     }
@@ -314,9 +315,10 @@ struct Queries {
     l += sum[0] + sum[1];
   }
   template <bool PAGES>
-  __device__ __forceinline__ void add(const TileLane<HD, PAGES>& at, const char* v, const Scores& s) {
+  __device__ __forceinline__ void add(const TileLane<HD, PAGES>& at, const char* v, const Scores& s, int n = N) {
 #pragma unroll
     for (int b = 0; b < 2 * N; ++b) {
+      if (b >= 2 * n) continue;
       const f32x16& p = s[b >> 1];
       const int r = 8 * (b & 1);
       // rounded to the type: 2^-9 (2^-12 in half precision) of a weight at most, of either sign, where the output's own rounding
