@@ -134,8 +134,9 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
     __syncthreads();
   };
   // A row's dS add up to 0 but for what the rounding of its output made of D: the keys' pass gets D with that taken back.  This pass
-  // cannot wait for it, and holds dS in pairs of numbers of the type instead (errors relative to the gradient of bf16 inputs of 279
-  // rows, whose own rounding is 1.66e-3: of dk 2.7e-3 with neither, 2.3e-3 with D; of dq 2.8e-3 with neither, 2.2e-3 with pairs).
+  // cannot wait for it but for the first rows, where dS is smallest beside D, and holds dS in pairs of numbers of the type instead
+  // (errors relative to the gradient of bf16 inputs of 279 rows, whose own rounding is 1.66e-3: of dk 2.7e-3 with neither, 2.3e-3 with
+  // D; of dq 2.8e-3 with neither, 2.2e-3 with pairs).
   float excess = 0.f;
   // dS of the 32 keys from 32 t on of the tile in buffer `parity`, before the scale; keys behind `to` (from the tile's first) none
   auto ds_of = [&](int parity, int t, int to, bool count) {
@@ -167,6 +168,12 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   if (own < 0) return;
   copy(j - 1, ~j & 1);
   const int to = min(qi - kTile * j, kTile - 1), halves = q0 % kTile / 32 + 1;  // of the own tile, those with keys that some query sees
+  if (j == 0) {  // all keys of these queries: D is exact before dS is taken
+#pragma nounroll
+    for (int t = 0; t < halves; ++t) ds_of(j & 1, t, to, true);
+    d += half_sum(excess);
+    excess = 0.f;
+  }
 #pragma nounroll
   for (int t = 0; t < halves; ++t) {
     f32x16 s = ds_of(j & 1, t, to, true);
@@ -363,7 +370,7 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   }
   if ((lane & 31) >= n) return;
   const int64_t width = (int64_t)a.n_kv_heads * HD;
-  float* to = kp.sums + 2 * part * a.rows * width + row * width + kvh * HD + 4 * h;
+  float* to = kp.sums + (2 * (int64_t)part * a.rows + row) * width + kvh * HD + 4 * h;
 #pragma unroll
   for (int mb = 0; mb < HD / 32; ++mb)
 #pragma unroll
