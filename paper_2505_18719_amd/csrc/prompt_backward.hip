@@ -4,8 +4,9 @@
 //            dQ^T += K^T dS^T
 //   keys:    a wave holds 32 keys as columns and goes over the queries behind them, of every head that reads the keys:
 //            S = Q K^T, dP = dO V^T - D, dV^T += dO^T P, dK^T += Q^T dS
-// Bound: the matrix units.  The gradient is 10 head_dim flops a query-key pair; scores and dP are computed in both passes, which
-// makes 14.  Each tile lies in LDS once, read by rows for one product and transposed for the other.
+// Bound: the matrix units.  The gradient is 10 head_dim flops a query-key pair; scores and dP are computed in both passes and dS
+// enters dQ as a pair, which makes 16 (3001 to 5003 rows, 16 on 4 heads of 128: 0.83 PFLOP/s of those, 0.52 of the 10).  Each tile
+// lies in LDS once, read by rows for one product and transposed for the other.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -419,12 +420,14 @@ __global__ __launch_bounds__(kSumThreads) void prompt_sum_kernel(PromptBwdArgs b
 // ------------------------------------------------------------------ host
 constexpr int kWaves = 4;
 
-// Parts of each 128 keys' queries: enough to fill the GPU twice over, as the first keys of a sequence have many times the work of the
-// last ones.
+// Parts of each 128 keys' queries.  Where the keys' workgroups leave CUs idle, as many as fill the GPU once, with two tiles each or more (16
+// sequences of 54 to 108 rows, 16 on 2 heads of 256: 87 us, whole 132; 1400 rows of 8 heads of 128: 91, in two parts 101, in ten 112).
+// Long ones, eight tiles or more to a part, fill it twice over, as the first keys of a sequence have many times the work of the last ones.
 int key_parts(int rows, int n_seq, int n_heads, int n_kv_heads) {
   const long long groups = seq_items<kWaves>(rows, n_seq, 1) * n_kv_heads;
   const long long steps = ((long long)rows / n_seq / kTile + 1) * (n_heads / n_kv_heads);  // of a workgroup, about
-  return (int)std::max(1ll, std::min({1024 / groups, steps / 8, 16ll}));
+  const long long once = steps < 6 ? 1 : std::min(512 / groups, steps / 2), twice = std::min(1024 / groups, steps / 8);
+  return (int)std::max(1ll, std::min(std::max(once, twice), 16ll));
 }
 size_t stat_bytes(int rows, int n_heads) { return ((size_t)rows * n_heads * sizeof(float2) + 255) / 256 * 256; }
 
