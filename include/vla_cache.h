@@ -6,8 +6,11 @@
  *     vla_qk_norm_rope       per layer: head norms and rotation of q and k,
  *                            k and v appended to the cache
  *     vla_paged_attention    per layer: every environment's new token over
- *                            all of its cached tokens
+ *                            all of its cached tokens; vla_shared_attention
+ *                            where groups of environments begin alike
  * and vla_qk_norm_rope_backward is the gradient of the norms and rotation.
+ * vla_kv_append_f8, vla_kv_read_f8 and vla_paged_attention_f8 keep the cache
+ * in 8-bit numbers; attention over whole prompts is in vla_prompt.h.
  * None of them needs a model handle.  Where vla_prefill and
  * vla_decode_actions run a fixed decoder over at most 320 tokens, these take
  * grouped key heads, normed heads, partial, interleaved and scaled rotations,

@@ -14,10 +14,10 @@
  * into a graph, and calls on different streams may overlap if they share no
  * buffer that either writes.
  *
- * Scores, softmax statistics and sums are fp32; the softmax weights (and in
- * the gradient the weights times the scores' gradients) are rounded once to
- * `dtype` where they meet the other factor of their product, and each output
- * is rounded once, to nearest even.  The same bits every run.
+ * Scores, softmax statistics and sums are fp32.  Where they meet the other
+ * factor of a product, softmax weights are rounded once to `dtype`, as are the
+ * scores' gradients for dk; for dq they enter as pairs of numbers of `dtype`.
+ * Each output is rounded once, to nearest even.  The same bits every run.
  *
  * Sequence s holds rows row_start[s] .. row_start[s + 1] - 1 of q, k and v.
  * Its row i attends rows 0 .. i of it:
