@@ -5,10 +5,11 @@
 //   shared  takes 32 columns a wave, a column being one query head of one environment of a group, over a run of the group's shared
 //           pages, which pass through LDS in tiles of four as in attention over whole prompts
 //   own     takes an environment's remaining pages, or a run of them, as attention without sharing does
-// Each leaves its columns' maxima, sums of weights and sums of weighted values, and own ones say which parts there are none of, so that
-// the join has no lengths or groups to look up (its time for 128 environments of 8 groups: 4.8 us, was 6.6).  What bounds it in earnest is a wave's way through a
-// tile, 1.7 us with its SIMD to itself or shared with one (50 environments, 16384 shared tokens, 28 on 4 heads of 128: 39 us, of which
-// ten tiles a workgroup 17, the start 8, the parts' way through memory 5 and their sum 6; unshared 244).
+// Each leaves its columns' maxima, sums of weights and sums of weighted values, and own ones say which parts there are none of, so
+// that the join has no lengths or groups to look up (its time for 128 environments of 8 groups: 4.8 us, was 6.6).  What bounds it
+// in earnest is a wave's way through a tile, 1.7 us with its SIMD to itself or shared with one (50 environments, 16384 shared
+// tokens, 28 on 4 heads of 128: 38 us, of which ten tiles a workgroup 17, the start 8, the parts' way through memory 5 and their
+// sum 7; unshared 244).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
