@@ -320,11 +320,13 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
       dk.add(at, tile(n, 0), t, ds);
     }
   };
+  // Halves of tile j that have queries.
+  auto halves = [&](int j) { return kTile * j + 32 < st.len ? 2 : 1; };
   dk.begin();
   dv.begin();
   over(first, behind, [&](int n, int j) {
 #pragma nounroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < halves(j); ++t) {
       f32x16 p, ds;
       weights(n, t, kj - kTile * j, true, p, ds);
       add(n, t, p, ds);
@@ -339,7 +341,7 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
     over(first, behind, [&](int n, int j) {
       if (!spoiled) return;
 #pragma nounroll
-      for (int t = 0; t < 2; ++t) {
+      for (int t = 0; t < halves(j); ++t) {
         f32x16 p, ds;
         weights(n, t, kj - kTile * j, true, p, ds);
         if constexpr (DV) dv.add_only(tile(n, 1), t, p, kj - kTile * j, kTile);
@@ -352,7 +354,7 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   }
   over(behind, end, [&](int n, int j) {
 #pragma nounroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < halves(j); ++t) {
       f32x16 p, ds;
       weights(n, t, 0, false, p, ds);
       add(n, t, p, ds);
