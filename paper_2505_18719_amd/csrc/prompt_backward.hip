@@ -253,21 +253,25 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   const int own = k0 < st.len ? k0 / kTile : end;
   auto tile = [&](int n, int which) { return lds + (2 * (n & 1) + which) * kTileBytes<HD>; };
   auto stat = [&](int n) { return reinterpret_cast<float*>(lds + 4 * kTileBytes<HD>) + (n & 1) * 2 * kTile; };  // log-sum-exps, then D
+  // Halves of tile j that have queries.
+  auto halves = [&](int j) { return kTile * j + 32 < st.len ? 2 : 1; };
   // Tile j of head `head` into buffer n.  Its rows' statistics pass through a register of the first wave, which puts them there after
-  // the tile before has been used: rows behind the last have weights of 0.
+  // the tile before has been used: rows behind the last have weights of 0.  (Their lanes load too: where a branch leaves lanes out, the
+  // compiler has been seen to save registers of all lanes before it takes them in again.)
   float2 x = make_float2(INFINITY, 0.f);
+  int n_stat = 0;
   auto copy = [&](int n, int head, int j) {
     const SeqRows q = {a.q.p + st.row0 * a.q.ld + head * HD, a.q.ld};
     const SeqRows go = {b.dout.p + st.row0 * b.dout.ld + head * HD, b.dout.ld};
     copy_tile<HD, NW>(tile(n, 0), q, kTile * j, st.len, wave);
     copy_tile<HD, NW>(tile(n, 1), go, kTile * j, st.len, wave);
-    const int i = kTile * j + lane;
-    if (wave == 0) x = i < st.len ? stats[(int64_t)head * a.rows + st.row0 + i] : make_float2(INFINITY, 0.f);
+    n_stat = st.len - kTile * j;
+    if (wave == 0) x = stats[(int64_t)head * a.rows + st.row0 + min(kTile * j + lane, st.len - 1)];
   };
   auto arrived = [&](int n) {
     if (wave == 0) {
-      stat(n)[lane] = x.x;
-      stat(n)[kTile + lane] = x.y;
+      stat(n)[lane] = lane < n_stat ? x.x : INFINITY;
+      stat(n)[kTile + lane] = lane < n_stat ? x.y : 0.f;
     }
     WAIT_VMCNT(0);
     __syncthreads();
@@ -320,8 +324,6 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
       dk.add(at, tile(n, 0), t, ds);
     }
   };
-  // Halves of tile j that have queries.
-  auto halves = [&](int j) { return kTile * j + 32 < st.len ? 2 : 1; };
   dk.begin();
   dv.begin();
   over(first, behind, [&](int n, int j) {
