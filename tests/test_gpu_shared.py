@@ -226,3 +226,25 @@ def test_samples_of_one_observation_step_by_step():
         got = vla.shared_attention(q, kp, vp, tables, lens, start, shared, 0.125)
         ref, _, mag, smax = co.paged_attention(f64(q), f64(kp), f64(vp), tables.cpu().numpy(), lens.cpu().numpy(), 0.125)
         assert np.all(np.abs(f64(got) - ref) <= attn_tol(ref, mag, smax, hd, BF) + mag * 2.0 ** -9)
+
+
+@pytest.mark.parametrize("H", [1, 3])
+def test_most_environments(H):
+    """65535 environments, the most that a call takes, in groups of 2 and 3 over 50 pages that all share; some against 64 bits."""
+    n, hd, scale = 65535, 64, 0.125
+    start = np.concatenate([np.arange(0, 60000, 2), np.arange(60000, n, 3), [n]])
+    rng = np.random.default_rng(3)
+    shared = rng.integers(1, 4, len(start) - 1)
+    group = np.repeat(np.arange(len(shared)), np.diff(start))
+    lens = PAGE * shared[group] + rng.integers(0, 17, n)
+    table = rng.integers(0, 50, (len(shared), 3))[group]
+    table = np.concatenate([table, np.zeros((n, 1), table.dtype)], 1)
+    table[np.arange(n), shared[group]] = rng.integers(0, 50, n)
+    kp, vp, q = rand((50, 1, PAGE, hd), BF, 1), rand((50, 1, hd, PAGE), BF, 2), rand((n, H, hd), BF, 3, 2.0)
+    got = f64(vla.shared_attention(q, kp, vp, i32(table), i32(lens), i32(start), i32(shared), scale))
+    some = np.concatenate([np.arange(100), np.arange(59950, 60050), np.arange(n - 100, n)])
+    ref, _, mag, smax = co.paged_attention(f64(q)[some], f64(kp), f64(vp), table[some], lens[some], scale)
+    tol = attn_tol(ref, mag, smax, hd, BF) + mag * (torch.finfo(BF).eps / 2 + lens.max() * U32)
+    assert np.all(np.abs(got[some] - ref) <= tol)
+    whole = f64(vla.paged_attention(q, kp, vp, i32(table), i32(lens), scale))
+    assert np.isfinite(got).all() and np.abs(got - whole).max() < 0.1  # no row of another environment
