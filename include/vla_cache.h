@@ -211,8 +211,10 @@ int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int3
  *                 not ascend, the results are left open)
  *   shared_pages  int32 [n_groups]: below 0 counts as 0, above max_pages as it
  *   workspace     vla_shared_attention_workspace_size bytes, 256-byte aligned
- * n_groups at most 65535.  Where groups have fewer than two environments in
- * the mean, nothing is gained, and nothing is shared. */
+ * n_env, as of every attention here, and n_groups at most 65535.  Where groups
+ * have fewer than two environments in the mean, nothing is gained, and nothing
+ * is shared; where all that vla_paged_attention would read lies in the GPU's
+ * caches (up to about 100 MB), that is as quick. */
 int vla_shared_attention_workspace_size(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads,
                                         int32_t head_dim, int32_t max_pages, size_t* bytes_host);
 int vla_shared_attention(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
