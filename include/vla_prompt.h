@@ -25,8 +25,9 @@
  * with head h reading key head h n_kv_heads / n_heads (rounded down).  Rows of
  * no sequence are neither read nor written: those before the first and behind
  * the last, and those of a sequence whose bounds descend or lie outside
- * [0, rows] (row_start ascends otherwise; where it does not, which of the
- * sequences that share a row writes it is left open).
+ * [0, rows].  Of up to 512 sequences such bounds change nothing for the
+ * others; more have to ascend within [0, rows].  What the rows of sequences
+ * get where these do not, or where sequences share rows, is left open.
  * Infinite and NaN elements reach what the formulas say they reach and nothing
  * else: no earlier row's outputs and no later key's gradients; whether they
  * arrive as an infinity or as NaN is left open.  A head all of whose scores

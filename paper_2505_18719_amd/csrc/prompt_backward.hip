@@ -399,19 +399,18 @@ __global__ __launch_bounds__(kSumThreads) void prompt_sum_kernel(PromptBwdArgs b
   const int64_t i = (int64_t)blockIdx.x * kSumThreads + threadIdx.x, row = i / (width / 4);
   const int f = 4 * (int)(i % (width / 4));
   if (row >= a.rows) return;
-  // the last sequence that begins at or before the row
-  int lo = 0, n = a.n_seq;
-  while (n > 1) {
-    const int half = n / 2;
-    if (a.row_start[lo + half] <= row) {
-      lo += half;
-      n -= half;
-    } else {
-      n = half;
+  bool in = false;  // a row of a sequence (fewer than 410 of them: more fill the GPU, and their keys have one part)
+  for (int s = 0, start = a.row_start[0]; s < a.n_seq; s += 8) {
+    int end[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) end[i] = a.row_start[min(s + 1 + i, a.n_seq)];  // behind the last: an empty one
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      in |= start >= 0 && start <= row && row < end[i] && end[i] <= a.rows;
+      start = end[i];
     }
   }
-  const int start = a.row_start[lo], end = a.row_start[lo + 1];
-  if (start < 0 || start > row || end <= row || end > a.rows) return;
+  if (!in) return;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
     f32x4 s = {0.f, 0.f, 0.f, 0.f};

@@ -333,8 +333,10 @@ struct Queries {
 
 // ------------------------------------------------------------------ from a workgroup to its rows
 // A wave takes a block of 32 rows of one of `group` heads: a sequence's blocks and heads lie in a line, block by block, of which
-// a workgroup takes NW, so that its waves have keys alike, and none idles but for a sequence's last item.  Sequence s has items
-// first_item(row_start[s], s) and on: enough of them, and none of the next sequence's, whatever the lengths, so that a workgroup
+// a workgroup takes NW, an item, so that its waves have keys alike, and none idles but for a sequence's last item.  A sequence whose
+// bounds descend or lie outside [0, rows] has no items.  Up to kListed * 64 sequences are all looked at by every wave, so that such
+// bounds cost the others nothing.  Of more, sequence s has
+// items first_item(row_start[s], s) and on, enough of them and none of the next sequence's if the bounds ascend, so that a workgroup
 // finds its sequence by a search of row_start; the items in between are empty.
 struct SeqItem {
   int row0, len, nth;  // first row and rows of the sequence, the item's place in it from the last one back
@@ -343,12 +345,79 @@ template <int NW>
 __host__ __device__ __forceinline__ long long first_item(int start, int s, int group) {
   return ((long long)(start / 32) + s) * group / NW + s;
 }
+// Items of a launch: of sequences that share no row never fewer than there are, whatever their order.
 template <int NW>
 long long seq_items(int rows, int n_seq, int group) { return first_item<NW>(rows, n_seq, group); }
+template <int NW>
+__device__ __forceinline__ int items_of(int len, int group) {  // 32 bits: prompt_fits
+  return (int)(((unsigned)(len + 31) / 32 * (unsigned)group + NW - 1) / NW);
+}
+
+// Sum over the lanes up to each, and over all.
+__device__ __forceinline__ unsigned wave_upto(unsigned v) {
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x111, 0xF, 0xF, false);  // the lane 1, 2, 4, 8 before in its 16
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x112, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x114, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x118, 0xF, 0xF, false);
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x142, 0xA, 0xF, false);  // lane 15 to the second 16 (47 to the fourth)
+  v += __builtin_amdgcn_update_dpp(0, (int)v, 0x143, 0xC, 0xF, false);  // lane 31 to the second 32
+  return v;
+}
+__device__ __forceinline__ unsigned wave_total(unsigned v) { return (unsigned)__builtin_amdgcn_readlane(wave_upto(v), kWave - 1); }
+
+// Sequences 64 p + lane, p = 0 .. kListed - 1: rows (none of one to be passed over) and items.
+constexpr int kListed = 8, kListedSeqs = kListed * kWave;
+constexpr int kMostItems = 1 << 25;  // above every item of a launch (prompt_fits): sums of lanes' items, held to it, fit 32 bits
+struct SeqList {
+  int start[kListed], len[kListed], items[kListed];
+};
+template <int NW>
+__device__ __forceinline__ void list_sequences(const int32_t* row_start, int n_seq, int rows, int group, SeqList& q) {
+  auto look = [&](int p) {
+    const int s = p * kWave + (threadIdx.x & 63), from = row_start[min(s, n_seq)], to = row_start[min(s + 1, n_seq)];
+    const bool usable = s < n_seq && from >= 0 && from < to && to <= rows;
+    q.start[p] = from;
+    q.len[p] = usable ? to - from : 0;
+    q.items[p] = items_of<NW>(q.len[p], group);
+  };
+  look(0);
+#pragma unroll
+  for (int p = 1; p < kListed; ++p) q.start[p] = q.len[p] = q.items[p] = 0;
+  if (n_seq > kWave) {
+#pragma unroll
+    for (int p = 1; p < kListed; ++p) look(p);
+  }
+}
 
 template <int NW>
 __device__ __forceinline__ bool find_item(const int32_t* row_start, int n_seq, int rows, int group, int item, SeqItem& t) {
   const int lane = threadIdx.x & 63;
+  if (n_seq <= kListedSeqs) {  // items lane by lane
+    SeqList q;
+    list_sequences<NW>(row_start, n_seq, rows, group, q);
+    int mine = q.items[0];
+#pragma unroll
+    for (int p = 1; p < kListed; ++p) mine = min(mine + q.items[p], kMostItems);
+    const unsigned upto = wave_upto(mine);
+    const int l = __popcll(__ballot(upto <= (unsigned)item));
+    if (l == kWave) return false;
+    int left = item - (int)(__builtin_amdgcn_readlane(upto, l) - __builtin_amdgcn_readlane(mine, l));  // items from the lane's first on
+    int start = q.start[0], len = q.len[0], items = __builtin_amdgcn_readlane(q.items[0], l);
+    if (n_seq > kWave) {
+#pragma unroll
+      for (int p = 1; p < kListed; ++p) {
+        if (left < items) continue;
+        left -= items;
+        start = q.start[p];
+        len = q.len[p];
+        items = __builtin_amdgcn_readlane(q.items[p], l);
+      }
+    }
+    t.row0 = __builtin_amdgcn_readlane(start, l);
+    t.len = __builtin_amdgcn_readlane(len, l);
+    t.nth = items - 1 - left;  // the longest rows of a sequence first
+    return true;
+  }
   int lo = 0, n = n_seq, start, end;
   for (;;) {
     const int step = (n + kWave - 1) / kWave, at = min(lo + lane * step, n_seq), v = row_start[at];
@@ -366,72 +435,51 @@ __device__ __forceinline__ bool find_item(const int32_t* row_start, int n_seq, i
   end = __builtin_amdgcn_readfirstlane(end);
   if (t.row0 < 0 || end <= t.row0 || end > rows) return false;
   t.len = end - t.row0;
-  const int items = (int)(((long long)((t.len + 31) / 32) * group + NW - 1) / NW);
+  const int items = items_of<NW>(t.len, group);
   const int nth = item - (int)first_item<NW>(t.row0, __builtin_amdgcn_readfirstlane(lo), group);
-  t.nth = items - 1 - nth;  // the longest rows of a sequence first
-  return nth < items;
+  t.nth = items - 1 - nth;
+  return nth >= 0 && nth < items;
 }
 
-// Sum over the wave.
-__device__ __forceinline__ int wave_total(int v) {
-  v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xF, 0xF, false);  // the lane 1, 2, 4, 8 before in its 16
-  v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xF, 0xF, false);
-  v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xA, 0xF, false);  // lane 15 to the second 16 (47 to the fourth)
-  v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xC, 0xF, false);  // lane 31 to the second 32
-  return __builtin_amdgcn_readlane(v, kWave - 1);
-}
-
-// As find_item, but of up to 512 sequences the items of all in the order of their length, the longest first, so that no long one
-// starts late: an item's place in its sequence says how long it is, and every sequence has one of each length up to its number of items.
-// Costs a workgroup about 1 us: worth it where a workgroup takes many times that.
-constexpr int kSorted = 8;
+// As find_item, but of up to kListedSeqs sequences the items of all in the order of their length, the longest first, so that no long
+// one starts late: an item's place in its sequence says how long it is, and every sequence has one of each length up to its number of
+// items.  Costs a workgroup about 1 us: worth it where a workgroup takes many times that.
 template <int NW>
 __device__ __forceinline__ bool find_sorted(const int32_t* row_start, int n_seq, int rows, int group, int item, SeqItem& t) {
-  if (n_seq > kSorted * kWave) return find_item<NW>(row_start, n_seq, rows, group, item, t);
+  if (n_seq > kListedSeqs) return find_item<NW>(row_start, n_seq, rows, group, item, t);
   const int lane = threadIdx.x & 63;
-  int start[kSorted], len[kSorted], items[kSorted], most = 0, total = 0;
+  SeqList q;
+  list_sequences<NW>(row_start, n_seq, rows, group, q);
+  int most = 0;
 #pragma unroll
-  for (int p = 0; p < kSorted; ++p) {
-    start[p] = len[p] = items[p] = 0;
-    if (p * kWave >= n_seq) continue;
-    const int s = p * kWave + lane, from = row_start[min(s, n_seq)], to = row_start[min(s + 1, n_seq)];
-    if (s < n_seq && from >= 0 && from < to && to <= rows) {
-      start[p] = from;
-      len[p] = to - from;
-      items[p] = (int)(((long long)((len[p] + 31) / 32) * group + NW - 1) / NW);
-    }
-    most = max(most, items[p]);
-    total += items[p];
-  }
-  if (wave_total(total) <= item) return false;
+  for (int p = 0; p < kListed; ++p) most = max(most, q.items[p]);
   // items of length w or more
   auto from_length = [&](int w) {
     int n = 0;
 #pragma unroll
-    for (int p = 0; p < kSorted; ++p)
-      if (p * kWave < n_seq) n += max(items[p] - w + 1, 0);
+    for (int p = 0; p < kListed; ++p)
+      if (p * kWave < n_seq) n = min(n + max(q.items[p] - w + 1, 0), kMostItems);
     return wave_total(n);
   };
+  if (from_length(1) <= (unsigned)item) return false;
   int w = 1, hi = 1;
   while (__any(most >= 2 * hi)) hi *= 2;
   for (int bit = hi; bit > 0; bit /= 2)
-    if (from_length(w + bit) > item) w += bit;
-  int rank = item - from_length(w + 1);
+    if (from_length(w + bit) > (unsigned)item) w += bit;
+  int rank = item - (int)from_length(w + 1);
   bool found = false;
 #pragma unroll
-  for (int p = 0; p < kSorted; ++p) {
+  for (int p = 0; p < kListed; ++p) {
     if (p * kWave >= n_seq || found) continue;
-    const unsigned long long has = __ballot(items[p] >= w);
+    const unsigned long long has = __ballot(q.items[p] >= w);
     if (rank >= __popcll(has)) {
       rank -= __popcll(has);
       continue;
     }
-    const bool it = items[p] >= w && __popcll(has & ((1ull << lane) - 1)) == rank;
+    const bool it = q.items[p] >= w && __popcll(has & ((1ull << lane) - 1)) == rank;
     const int l = __builtin_ctzll(__ballot(it));
-    t.row0 = __builtin_amdgcn_readlane(start[p], l);
-    t.len = __builtin_amdgcn_readlane(len[p], l);
+    t.row0 = __builtin_amdgcn_readlane(q.start[p], l);
+    t.len = __builtin_amdgcn_readlane(q.len[p], l);
     found = true;
   }
   t.nth = w - 1;
