@@ -30,8 +30,9 @@
  * get where these do not, or where sequences share rows, is left open.
  * Infinite and NaN elements reach what the formulas say they reach and nothing
  * else: no earlier row's outputs and no later key's gradients; whether they
- * arrive as an infinity or as NaN is left open.  A head all of whose scores
- * are -inf gives zeros, also as gradients.
+ * arrive as an infinity or as NaN is left open.  A row's head all of whose
+ * scores are -inf gets zeros in out and dq and has no part in dk and dv,
+ * whatever its elements of q and dout are.
  */
 #ifndef VLA_PROMPT_H_
 #define VLA_PROMPT_H_

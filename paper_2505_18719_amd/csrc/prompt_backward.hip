@@ -20,11 +20,10 @@ namespace {
 
 using namespace tiles;
 
-// Of a query: its log-sum-exp to base 2 (+inf where it has no score above -inf: all weights 0), and D.
-struct RowStat {
-  float lse, d;
-};
-__device__ __forceinline__ float lse_base2(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+// A query's log-sum-exp to base 2; kNoWeight where it has no score above -inf.  Its weights are 0, and it is left out of all sums,
+// whatever its elements are.
+constexpr float kNoWeight = INFINITY;
+__device__ __forceinline__ float lse_base2(float lse) { return lse == -INFINITY ? kNoWeight : lse * kLog2e; }
 
 // Products with a column's weights, of any size, in the type's range.  In bf16 as they are.  Half precision has 5 bits of exponent:
 // each column's weights are held times a power of two that keeps the largest so far below 2^15 (and at first within a factor of four
@@ -80,9 +79,10 @@ struct Column {
       }
     }
   }
-  // The same with only the rows from `first` to `last` of the tile.
-  __device__ __forceinline__ void add_only(const char* tile, int t, const f32x16& w, int first, int last) {
-    add_apart<HD, T>(sum, w, tile, 32 * t, [&](int k) { return first <= k && k <= last; });
+  // The same with only the rows of the tile that are to be kept.
+  template <class F>
+  __device__ __forceinline__ void add_only(const char* tile, int t, const f32x16& w, F keep) {
+    add_apart<HD, T>(sum, w, tile, 32 * t, keep);
   }
 };
 
@@ -119,6 +119,8 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   }
   d = half_sum(d);
   const float lse = lse_base2(a.lse[row * a.n_heads + head]);
+  const bool none = lse == kNoWeight;
+  if (none) d = 0.f;
   Column<HD, T> dq;
   dq.begin();
   const TileLane<HD> at;
@@ -187,7 +189,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
     for (int t = 0; t < halves; ++t) {
       f32x16 s = ds_of(j & 1, t, to, false);
       dq.fit(s);
-      dq.add_only(keys(j & 1), t, s, 0, to);
+      dq.add_only(keys(j & 1), t, s, [&](int key) { return key <= to; });
     }
   }
   arrived();
@@ -210,7 +212,13 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
     tile(j - 1, 0);
   }
   excess = half_sum(excess);
-  if (mine && lane < 32) stats[(int64_t)head * a.rows + row] = make_float2(lse, d + excess);
+  if (mine && lane < 32) stats[(int64_t)head * a.rows + row] = make_float2(lse, none ? 0.f : d + excess);
+  if (__any(none)) {  // weights of 0 times keys of any size
+#pragma unroll
+    for (int i = 0; i < HD / 32; ++i)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dq.sum[i][r] = none ? 0.f : dq.sum[i][r];
+  }
   constexpr int kShare = 4 * kTileBytes<HD> / NW;
   store_rows<HD, T, kShare>(lds + wave * kShare, b.dq.p + (st.row0 + (int64_t)q0) * b.dq.ld + head * HD, b.dq.ld, min(st.len - q0, 32), dq.sum,
                             a.scale / dq.unit);
@@ -225,16 +233,19 @@ struct KeyParts {
 
 // WHAT: 1 dK, 2 dV, 3 both.  At head_dim 256 the sums of one alone fill half the registers: each has a launch of its own there, and
 // scores are computed once more.
-template <int HD, CacheType T, int NW, int WHAT>
-__global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats, KeyParts kp) {
-  extern __shared__ __align__(16) char lds[];
+//
+// Returns whether this wave's sums have a NaN; then they are not stored.  A weight of 0 times an infinite or NaN element may have
+// spoiled them: of a masked query, or of one without weight.  CAREFUL, for waves that are to go `again`, leaves such queries out: tiles
+// that have some are taken apart.
+template <int HD, CacheType T, int NW, int WHAT, bool CAREFUL>
+__device__ __forceinline__ bool keys_pass(const PromptBwdArgs& b, const float2* stats, const KeyParts& kp, char* lds, bool again) {
   constexpr int M = 32 * NW, KS = HD / 16;
   constexpr bool DK = WHAT & 1, DV = WHAT & 2;
   const PromptArgs& a = b.fwd;
   const int kvh = blockIdx.x % a.n_kv_heads, rest = blockIdx.x / a.n_kv_heads, part = rest % kp.parts, item = rest / kp.parts;
   const int group = a.n_heads / a.n_kv_heads;
   SeqItem st;
-  if (!find_sorted<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return;
+  if (!find_sorted<NW>(a.row_start, a.n_seq, a.rows, 1, item, st)) return false;
   const int lane = threadIdx.x & 63, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int nth = (st.len + M - 1) / M - 1 - st.nth;  // the first keys have the most queries
   const int k0 = M * nth + 32 * wave, kj = k0 + (lane & 31);
@@ -258,7 +269,7 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   // Tile j of head `head` into buffer n.  Its rows' statistics pass through a register of the first wave, which puts them there after
   // the tile before has been used: rows behind the last have weights of 0.  (Their lanes load too: where a branch leaves lanes out, the
   // compiler has been seen to save registers of all lanes before it takes them in again.)
-  float2 x = make_float2(INFINITY, 0.f);
+  float2 x = make_float2(kNoWeight, 0.f);
   int n_stat = 0;
   auto copy = [&](int n, int head, int j) {
     const SeqRows q = {a.q.p + st.row0 * a.q.ld + head * HD, a.q.ld};
@@ -270,7 +281,7 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   };
   auto arrived = [&](int n) {
     if (wave == 0) {
-      stat(n)[lane] = lane < n_stat ? x.x : INFINITY;
+      stat(n)[lane] = lane < n_stat ? x.x : kNoWeight;
       stat(n)[kTile + lane] = lane < n_stat ? x.y : 0.f;
     }
     WAIT_VMCNT(0);
@@ -326,43 +337,52 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
   };
   dk.begin();
   dv.begin();
-  over(first, behind, [&](int n, int j) {
+  if constexpr (CAREFUL) {
 #pragma nounroll
-    for (int t = 0; t < halves(j); ++t) {
-      f32x16 p, ds;
-      weights(n, t, kj - kTile * j, true, p, ds);
-      add(n, t, p, ds);
-    }
-  });
-  const bool spoiled = (DK && any_nan(dk.sum)) || (DV && any_nan(dv.sum));
-  if (__builtin_expect(__builtin_amdgcn_readfirstlane(__syncthreads_or(spoiled)), 0)) {  // masked queries may have spoiled the sums: once
-    if (spoiled) {                                                                        // more without them
-      dk.begin();
-      dv.begin();
-    }
+    for (int r = 0; r < 2; ++r)  // as the pass before divides them among the parts
+      over(r == 0 ? first : behind, r == 0 ? behind : end, [&](int n, int j) {
+        if (!again) return;
+        const bool apart = r == 0 || __any(lane < st.len - kTile * j && stat(n)[lane] == kNoWeight);
+        const int from = kj - kTile * j;
+        auto keep = [&](int k) { return k >= from && stat(n)[k] != kNoWeight; };
+#pragma nounroll
+        for (int t = 0; t < halves(j); ++t) {
+          f32x16 p, ds;
+          weights(n, t, from, true, p, ds);
+          if (!apart) {
+            add(n, t, p, ds);
+            continue;
+          }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) ds[i] = keep(32 * t + mma_row(i, h)) ? ds[i] : 0.f;
+          if constexpr (DV) dv.add_only(tile(n, 1), t, p, keep);
+          if constexpr (DK) {
+            dk.fit(ds);
+            dk.add_only(tile(n, 0), t, ds, keep);
+          }
+        }
+      });
+    if (!again) return false;
+  } else {
     over(first, behind, [&](int n, int j) {
-      if (!spoiled) return;
 #pragma nounroll
       for (int t = 0; t < halves(j); ++t) {
         f32x16 p, ds;
         weights(n, t, kj - kTile * j, true, p, ds);
-        if constexpr (DV) dv.add_only(tile(n, 1), t, p, kj - kTile * j, kTile);
-        if constexpr (DK) {
-          dk.fit(ds);
-          dk.add_only(tile(n, 0), t, ds, kj - kTile * j, kTile);
-        }
+        add(n, t, p, ds);
+      }
+    });
+    over(behind, end, [&](int n, int j) {
+#pragma nounroll
+      for (int t = 0; t < halves(j); ++t) {
+        f32x16 p, ds;
+        weights(n, t, 0, false, p, ds);
+        add(n, t, p, ds);
       }
     });
   }
-  over(behind, end, [&](int n, int j) {
-#pragma nounroll
-    for (int t = 0; t < halves(j); ++t) {
-      f32x16 p, ds;
-      weights(n, t, 0, false, p, ds);
-      add(n, t, p, ds);
-    }
-  });
-  if (own == end) return;
+  if (own == end) return false;
+  if (!CAREFUL && __builtin_expect((DK && any_nan(dk.sum)) || (DV && any_nan(dv.sum)), 0)) return true;
   constexpr float kUnit = T == kBf16 ? 1.f : 0x1p-15f;
   const int64_t first_row = st.row0 + (int64_t)k0;
   const int n = min(st.len - k0, 32);
@@ -371,9 +391,9 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
     constexpr int kShare = 4 * kTileBytes<HD> / NW;
     if constexpr (DK) store_rows<HD, T, kShare>(lds + wave * kShare, b.dk.p + first_row * b.dk.ld + kvh * HD, b.dk.ld, n, dk.sum, mul);
     if constexpr (DV) store_rows<HD, T, kShare>(lds + wave * kShare, b.dv.p + first_row * b.dv.ld + kvh * HD, b.dv.ld, n, dv.sum, kUnit);
-    return;
+    return false;
   }
-  if ((lane & 31) >= n) return;
+  if ((lane & 31) >= n) return false;
   const int64_t width = (int64_t)a.n_kv_heads * HD;
   float* to = kp.sums + (2 * (int64_t)part * a.rows + row) * width + kvh * HD + 4 * h;
 #pragma unroll
@@ -389,6 +409,35 @@ __global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(
       if constexpr (DK) *reinterpret_cast<f32x4*>(to + 32 * mb + 8 * i) = u;
       if constexpr (DV) *reinterpret_cast<f32x4*>(to + a.rows * width + 32 * mb + 8 * i) = w;
     }
+  return false;
+}
+
+// By a call, so that the pass that all take has not its registers: at head_dim 128 and 256 it spilled 22 to 227 with the tiles taken
+// apart in the same function, now 13 and none (64 sequences of 279 to 311 rows, 32 on 8 heads of 128: 375 us, was 391).  At 64 there
+// are enough, and the call's stack would cost 1 to 6 us.
+typedef __attribute__((address_space(3))) char shared_char;
+template <class S>
+__device__ __forceinline__ S uniform(const S& s) {  // a call's arguments come in vector registers
+  uint32_t w[sizeof(S) / 4];
+  __builtin_memcpy(w, &s, sizeof(S));
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(S) / 4); ++i) w[i] = __builtin_amdgcn_readfirstlane(w[i]);
+  S u;
+  __builtin_memcpy(&u, w, sizeof(S));
+  return u;
+}
+template <int HD, CacheType T, int NW, int WHAT>
+__device__ __attribute__((noinline)) void keys_again(PromptBwdArgs b, const float2* stats, KeyParts kp, shared_char* lds, bool again) {
+  keys_pass<HD, T, NW, WHAT, true>(uniform(b), uniform(stats), uniform(kp), (char*)uniform(lds), __builtin_amdgcn_readfirstlane(again));
+}
+template <int HD, CacheType T, int NW, int WHAT>
+__global__ __launch_bounds__(64 * NW, HD <= 128 ? 2 : 1) void prompt_dkv_kernel(PromptBwdArgs b, const float2* stats, KeyParts kp) {
+  extern __shared__ __align__(16) char lds[];
+  const bool again = keys_pass<HD, T, NW, WHAT, false>(b, stats, kp, lds, false);
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(__syncthreads_or(again)), 0)) {
+    if constexpr (HD == 64) keys_pass<HD, T, NW, WHAT, true>(b, stats, kp, lds, again);
+    else keys_again<HD, T, NW, WHAT>(b, stats, kp, (shared_char*)lds, again);
+  }
 }
 
 // Adds the parts' sums in order, four features a thread, of the rows of sequences.
