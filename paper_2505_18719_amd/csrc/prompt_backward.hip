@@ -107,7 +107,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
 #pragma unroll
   for (int i = 0; i < KS; ++i) {
     const int f = head * HD + 16 * i + 8 * h;
-    q[i] = sc.turned(*reinterpret_cast<const uint4*>(a.q.p + row * a.q.ld + f));
+    q[i] = *reinterpret_cast<const uint4*>(a.q.p + row * a.q.ld + f);
     go[i] = *reinterpret_cast<const uint4*>(b.dout.p + row * b.dout.ld + f);
     const uint4 o = *reinterpret_cast<const uint4*>(a.o.p + row * a.o.ld + f);
     const uint32_t x[4] = {go[i].x, go[i].y, go[i].z, go[i].w}, y[4] = {o.x, o.y, o.z, o.w};
@@ -121,6 +121,7 @@ __global__ __launch_bounds__(64 * NW, HD == 256 ? 1 : 2) void prompt_dq_kernel(P
   const float lse = lse_base2(a.lse[row * a.n_heads + head]);
   const bool none = lse == kNoWeight;
   if (none) d = 0.f;
+  sc.template turn<T>(q);
   Column<HD, T> dq;
   dq.begin();
   const TileLane<HD> at;
@@ -254,9 +255,10 @@ __device__ __forceinline__ bool keys_pass(const PromptBwdArgs& b, const float2* 
   uint4 k[KS], v[KS];
 #pragma unroll
   for (int i = 0; i < KS; ++i) {
-    k[i] = sc.turned(*reinterpret_cast<const uint4*>(a.k.p + row * a.k.ld + kvh * HD + 16 * i + 8 * h));
+    k[i] = *reinterpret_cast<const uint4*>(a.k.p + row * a.k.ld + kvh * HD + 16 * i + 8 * h);
     v[i] = *reinterpret_cast<const uint4*>(a.v.p + row * a.v.ld + kvh * HD + 16 * i + 8 * h);
   }
+  sc.template turn<T>(k);
   Column<HD, T> dk, dv;
   const TileLane<HD> at;
   // Tiles of queries: those with the workgroup's keys' own, of which one has pairs of this wave's that are masked, and those behind.

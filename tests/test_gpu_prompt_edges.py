@@ -5,7 +5,7 @@ import torch
 
 from oracle import prompt_oracle as po
 from paper_2505_18719_amd import vla
-from test_gpu_cache import BF, FP, f64
+from test_gpu_cache import BF, FP, U32, f64, half_step
 from test_gpu_prompt import INF, NAN, Case, bits
 
 pytestmark = pytest.mark.gpu
@@ -95,3 +95,37 @@ def test_rows_without_weight_beside_bad_elements(dtype):
     for got, want in ((dk[s:-2, 1], g[1][s:-2, 1]), (dv[s:-2, 1], g[2][s:-2, 1]), (dk[s + 101:-2, 0], g[1][s + 101:-2, 0])):
         assert np.linalg.norm(got - want) <= 4 * torch.finfo(dtype).eps / 2 * np.linalg.norm(want)
     assert (f64(c.dq)[s + 250, 3] == 0).all()
+
+
+@pytest.mark.parametrize("hd,dtype,H,K", [(64, BF, 4, 2), (128, FP, 4, 2), (256, BF, 2, 2)])
+@pytest.mark.parametrize("value", [NAN, INF, -INF])
+@pytest.mark.parametrize("what", ["q", "k"])
+def test_scale_of_0_times_infinite_elements(what, value, hd, dtype, H, K):
+    """0 times an infinite or NaN element is NaN: a query's reaches its row, a key's the rows that see it, and their gradients;
+    all else is what it is without them."""
+    c, clean = (Case([50, 120], H, K, hd, dtype, seed=4, scale=0.0) for _ in range(2))
+    r, head = int(c.start[1]) + 70, 1
+    getattr(c, what)[r, head, 11] = value
+    for x in (c, clean):
+        x.run()
+        x.back()
+    rows, heads = np.arange(c.rows), np.arange(H)
+    hit = (rows[:, None] == r) & (heads == head) if what == "q" else (rows[:, None] >= r) & (heads // (H // K) == head)
+    hit &= c.inside[:, None]
+    group = np.arange(K) == (head * K // H if what == "q" else head)
+    hit_kv = c.inside[:, None] & (rows[:, None] >= c.start[1]) & group  # keys that a row that is hit sees
+    if what == "q":
+        hit_kv &= rows[:, None] <= r
+    for name, where in (("out", hit), ("lse", hit), ("dq", hit), ("dk", hit_kv), ("dv", hit_kv)):
+        got, want = f64(getattr(c, name)), f64(getattr(clean, name))
+        assert np.isnan(got[where]).all(), name
+        bound = 0.0
+        if name == "dv":
+            # All weights of row i of a sequence are 1 / (i + 1).  A wave's keys beside one that is reached are summed with them in
+            # fp32, else rounded to the type (half a step of each term), and both results are rounded once: half a step each.
+            mag = np.zeros(want.shape)
+            for a, b in zip(c.start, c.start[1:]):
+                terms = np.abs(f64(c.dout)[a:b]) / np.arange(1, b - a + 1)[:, None, None]
+                mag[a:b] = terms[::-1].cumsum(0)[::-1].reshape(b - a, K, H // K, hd).sum(2)
+            bound = 2 * half_step(want, dtype) * (1 + 2 ** -6) + mag * (torch.finfo(dtype).eps / 2 + 2 * 120 * H * U32)
+        assert (np.abs(got - want) <= bound)[~where & c.inside[:, None]].all(), name
