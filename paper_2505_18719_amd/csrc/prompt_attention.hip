@@ -49,6 +49,8 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
   auto values = [&](int parity) { return lds + (2 + parity) * kTileBytes<HD>; };
   auto copy_keys = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW>(keys(parity), k, kTile * j, st.len, wave); };
   auto copy_values = [&](int j, int parity) { if (j >= 0) copy_tile<HD, NW>(values(parity), v, kTile * j, st.len, wave); };
+  // Every wave comes to last + 1 barriers behind the first two: one with the end of each tile but the first of the sequence, and one
+  // before the outputs; those without queries have one with the end of each tile.
   auto arrived = [&] {
     WAIT_VMCNT(0);
     __syncthreads();
@@ -87,8 +89,10 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
 #pragma unroll
     for (int t = 0; t < kTile / 32; ++t) add_apart<HD, T>(w.o, s[t], values(j & 1), 32 * t, [&](int key) { return kTile * j + key <= qi; });
   }
-  if (j > 0) w.scores(at, keys(~j & 1), s);
-  arrived();
+  if (j > 0) {
+    w.scores(at, keys(~j & 1), s);
+    arrived();
+  }
   auto tile = [&](int j, int parity, typename Queries<HD, T>::Scores& s, typename Queries<HD, T>::Scores& next) {
     copy_keys(j - 2, parity);
     copy_values(j - 1, 1 - parity);
