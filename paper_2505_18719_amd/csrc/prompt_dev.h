@@ -197,28 +197,6 @@ __device__ __forceinline__ bool any_nan(const f32x16 (&acc)[N]) {
   return __any(__builtin_isnan((s[0] + s[1]) + (s[2] + s[3])));
 }
 
-// Writes this lane's column of acc, times `mul`, as a row of HD numbers of the type: 16 bytes per store, the two halves of the wave
-// in turn.
-template <int HD, CacheType T>
-__device__ __forceinline__ void store_row(bf16_t* row, const f32x16 (&acc)[HD / 32], float mul, bool write) {
-  const int h = (threadIdx.x & 63) >> 5;
-#pragma unroll
-  for (int mb = 0; mb < HD / 32; ++mb)
-#pragma unroll
-    for (int i = 0; i < 4; i += 2) {
-      uint32_t a[2], b[2];  // features 8 i + 4 h .. + 4, and eight on
-#pragma unroll
-      for (int e = 0; e < 2; ++e) {
-        a[e] = pack2<T>(acc[mb][4 * i + 2 * e] * mul, acc[mb][4 * i + 2 * e + 1] * mul);
-        b[e] = pack2<T>(acc[mb][4 * i + 4 + 2 * e] * mul, acc[mb][4 * i + 5 + 2 * e] * mul);
-      }
-      // lane half 0 gets features 8 i .. + 8, half 1 those eight on
-      const auto x = __builtin_amdgcn_permlane32_swap(a[0], b[0], false, false);
-      const auto y = __builtin_amdgcn_permlane32_swap(a[1], b[1], false, false);
-      if (write) *reinterpret_cast<uint4*>(row + 32 * mb + 8 * i + 8 * h) = make_uint4(x[0], y[0], x[1], y[1]);
-    }
-}
-
 // Writes the columns of acc, times each lane's `mul`, as `n` rows (at most 32) of HD numbers of the type: through BYTES of LDS of the
 // wave's own, so that a store writes whole rows (stores straight from the columns write 32 bytes of 32 rows).
 template <int HD, CacheType T, int BYTES>
