@@ -236,8 +236,8 @@ struct KeyParts {
 // scores are computed once more.
 //
 // Returns whether this wave's sums have a NaN; then they are not stored.  A weight of 0 times an infinite or NaN element may have
-// spoiled them: of a masked query, or of one without weight.  CAREFUL, for waves that are to go `again`, leaves such queries out: tiles
-// that have some are taken apart.
+// spoiled them: of a masked query, or of one without weight.  CAREFUL, for waves that are to go `again`, leaves such queries out: the
+// keys' own tiles are taken apart, and those behind if there is one without weight.
 template <int HD, CacheType T, int NW, int WHAT, bool CAREFUL>
 __device__ __forceinline__ bool keys_pass(const PromptBwdArgs& b, const float2* stats, const KeyParts& kp, char* lds, bool again) {
   constexpr int M = 32 * NW, KS = HD / 16;
@@ -337,33 +337,41 @@ __device__ __forceinline__ bool keys_pass(const PromptBwdArgs& b, const float2* 
       dk.add(at, tile(n, 0), t, ds);
     }
   };
+  auto apart = [&](int n, int j) {
+    if (!again) return;
+    const int from = kj - kTile * j;
+    auto keep = [&](int k) { return k >= from && stat(n)[k] != kNoWeight; };
+#pragma nounroll
+    for (int t = 0; t < halves(j); ++t) {
+      f32x16 p, ds;
+      weights(n, t, from, true, p, ds);
+#pragma unroll
+      for (int i = 0; i < 16; ++i) ds[i] = keep(32 * t + mma_row(i, h)) ? ds[i] : 0.f;
+      if constexpr (DV) dv.add_only(tile(n, 1), t, p, keep);
+      if constexpr (DK) {
+        dk.fit(ds);
+        dk.add_only(tile(n, 0), t, ds, keep);
+      }
+    }
+  };
+  auto whole = [&](int n, int j) {
+    if (CAREFUL && !again) return;
+#pragma nounroll
+    for (int t = 0; t < halves(j); ++t) {
+      f32x16 p, ds;
+      weights(n, t, 0, false, p, ds);
+      add(n, t, p, ds);
+    }
+  };
   dk.begin();
   dv.begin();
   if constexpr (CAREFUL) {
-#pragma nounroll
-    for (int r = 0; r < 2; ++r)  // as the pass before divides them among the parts
-      over(r == 0 ? first : behind, r == 0 ? behind : end, [&](int n, int j) {
-        if (!again) return;
-        const bool apart = r == 0 || __any(lane < st.len - kTile * j && stat(n)[lane] == kNoWeight);
-        const int from = kj - kTile * j;
-        auto keep = [&](int k) { return k >= from && stat(n)[k] != kNoWeight; };
-#pragma nounroll
-        for (int t = 0; t < halves(j); ++t) {
-          f32x16 p, ds;
-          weights(n, t, from, true, p, ds);
-          if (!apart) {
-            add(n, t, p, ds);
-            continue;
-          }
-#pragma unroll
-          for (int i = 0; i < 16; ++i) ds[i] = keep(32 * t + mma_row(i, h)) ? ds[i] : 0.f;
-          if constexpr (DV) dv.add_only(tile(n, 1), t, p, keep);
-          if constexpr (DK) {
-            dk.fit(ds);
-            dk.add_only(tile(n, 0), t, ds, keep);
-          }
-        }
-      });
+    over(first, behind, apart);
+    bool none = false;  // a query without weight behind the keys
+    for (int head = kvh * group; head < (kvh + 1) * group; ++head)
+      for (int i = kTile * behind + (int)threadIdx.x; i < st.len; i += 64 * NW) none |= stats[(int64_t)head * a.rows + st.row0 + i].x == kNoWeight;
+    if (__builtin_amdgcn_readfirstlane(__syncthreads_or(none))) over(behind, end, apart);
+    else over(behind, end, whole);
     if (!again) return false;
   } else {
     over(first, behind, [&](int n, int j) {
@@ -374,14 +382,7 @@ __device__ __forceinline__ bool keys_pass(const PromptBwdArgs& b, const float2* 
         add(n, t, p, ds);
       }
     });
-    over(behind, end, [&](int n, int j) {
-#pragma nounroll
-      for (int t = 0; t < halves(j); ++t) {
-        f32x16 p, ds;
-        weights(n, t, 0, false, p, ds);
-        add(n, t, p, ds);
-      }
-    });
+    over(behind, end, whole);
   }
   if (own == end) return false;
   if (!CAREFUL && __builtin_expect((DK && any_nan(dk.sum)) || (DV && any_nan(dv.sum)), 0)) return true;
