@@ -10,8 +10,6 @@
 // first that a wave takes is the one part of which is masked, all others are whole.
 #include <hip/hip_runtime.h>
 
-#include <algorithm>
-
 #include "lds_limit.h"
 #include "prompt.h"
 #include "prompt_dev.h"
@@ -128,37 +126,34 @@ __global__ __launch_bounds__(64 * NW, kWavesPerSimd<HD>) void prompt_attn_kernel
   if (a.lse && mine && lane < 32) a.lse[row * a.n_heads + head] = ((w.m * w.scale - kHeldExp<T>) + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <int HD, CacheType T, int NW>
+// Four waves share a tile's way through LDS, two workgroups a CU (64 x 272 to 304 rows, 32 heads of 128: 117 us, with two waves 179,
+// with eight 133; up to 8190 rows, 28 heads: 526, 775 and 513; one of 278: 10.6, 10.9 and 12.3; of 1400, 32 heads of 256: 70, with two
+// waves 115, which are faster only there and up to 100 rows, 8.2 for 9.1).
+constexpr int kWaves = 4;
+
+template <int HD, CacheType T>
 hipError_t launch(const PromptArgs& a, hipStream_t s) {
   static LdsLimit limit;
-  const auto kernel = prompt_attn_kernel<HD, T, NW>;
+  const auto kernel = prompt_attn_kernel<HD, T, kWaves>;
   constexpr int kLds = 4 * kTileBytes<HD>;
   const hipError_t e = limit.allow((const void*)kernel, kLds);
   if (e != hipSuccess) return e;
-  const long long groups = seq_items<NW>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads;
-  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * NW), kLds, s, a);
+  const long long groups = seq_items<kWaves>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)groups), dim3(64 * kWaves), kLds, s, a);
   return hipGetLastError();
-}
-
-template <int HD, CacheType T>
-hipError_t launch_rows(const PromptArgs& a, hipStream_t s) {
-  // Four waves share a tile's way through LDS, two workgroups a CU (64 x 272 to 304 rows, 32 heads: 129 us, with two waves 181, with
-  // eight 148; 8190 rows, 28 heads: 493, 688 and 487); where those do not fill the GPU, two are as fast or faster (one of 278: 10.5 us, 10.8).
-  if (seq_items<4>(a.rows, a.n_seq, a.n_heads / a.n_kv_heads) * a.n_kv_heads >= 512) return launch<HD, T, 4>(a, s);
-  return launch<HD, T, 2>(a, s);
 }
 
 template <CacheType T>
 hipError_t launch_type(const PromptArgs& a, hipStream_t s) {
-  if (a.head_dim == 64) return launch_rows<64, T>(a, s);
-  if (a.head_dim == 128) return launch_rows<128, T>(a, s);
-  if (a.head_dim == 256) return launch_rows<256, T>(a, s);
+  if (a.head_dim == 64) return launch<64, T>(a, s);
+  if (a.head_dim == 128) return launch<128, T>(a, s);
+  if (a.head_dim == 256) return launch<256, T>(a, s);
   return hipErrorInvalidValue;
 }
 
 }  // namespace
 
-bool prompt_fits(int rows, int n_seq, int n_heads) {  // threads of the most workgroups that there can be, of two waves
+bool prompt_fits(int rows, int n_seq, int n_heads) {  // threads of the most workgroups of any of the kernels, below 2^32
   return n_seq < 1 << 26 && (tiles::seq_items<2>(rows, n_seq, 1) + n_seq) * n_heads * 128 < 1ll << 32;
 }
 
