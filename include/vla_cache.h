@@ -205,7 +205,8 @@ int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int3
  * environment.  Arguments and results otherwise as vla_paged_attention's, but
  * that the weights of shared pages are rounded once to `dtype`, that infinite
  * and NaN elements there arrive as an infinity or as NaN, which is left open,
- * and that an environment shorter than its group's pages gets NaN.
+ * and that an environment shorter than its group's pages gets NaN where pages
+ * are shared.
  *   group_start   int32 [n_groups + 1], ascending from 0 or more to n_env or
  *                 less; environments of no group share nothing (where it does
  *                 not ascend, the results are left open)
@@ -213,8 +214,12 @@ int vla_paged_attention(int32_t n_env, int32_t n_heads, int32_t n_kv_heads, int3
  *   workspace     vla_shared_attention_workspace_size bytes, 256-byte aligned
  * n_env, as of every attention here, and n_groups at most 65535.  Where groups
  * have fewer than two environments in the mean, nothing is gained, and nothing
- * is shared; where all that vla_paged_attention would read lies in the GPU's
- * caches (up to about 100 MB), that is as quick. */
+ * is shared.  vla_paged_attention is faster where all that it would read lies
+ * in the GPU's caches (128 environments in 8 groups that share 304 tokens, 32
+ * on 8 heads of 128: 12 us, this 15), and where most of what is read is not
+ * shared: an environment's own pages are divided among workgroups by the
+ * number of environments and the table's columns alone (64 of 1000 to 8000
+ * tokens, two of which share 960: 178 us, this 244). */
 int vla_shared_attention_workspace_size(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads,
                                         int32_t head_dim, int32_t max_pages, size_t* bytes_host);
 int vla_shared_attention(int32_t n_env, int32_t n_groups, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,

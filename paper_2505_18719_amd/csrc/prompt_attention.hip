@@ -1,9 +1,9 @@
 // Causal attention over whole prompts (vla_prompt_attention).
 //
 // Bound: the matrix units, 4 head_dim flops a query-key pair, and beside them the vector units, which take an exponential, a
-// product, a maximum, a sum and a rounding of each pair's score (8190 rows, 28 on 4 heads of 128: 0.99 PFLOP/s, where a large
+// product, a maximum, a sum and a rounding of each pair's score (8190 rows, 28 on 4 heads of 128: 0.9 to 1.0 PFLOP/s, where a large
 // product reaches 1.5; matrix units and vector units busy 57 % of the time each).  Short sequences are bound by a workgroup's way
-// in and out: of 129 us for 64 of 272 to 304 rows, 32 on 8 heads, 55 are queries and first tiles, 30 the outputs.  A wave holds 32
+// in and out: of 117 us for 64 of 272 to 304 rows, 32 on 8 heads, 39 are queries and first tiles, 30 the outputs.  A wave holds 32
 // queries of one head as MFMA columns, its workgroup's waves 32 queries each further on; tiles of 64 keys and values pass through
 // LDS, the next on its way while one is used.  S^T = K Q^T leaves a query's scores in two lanes, so that the running maximum costs
 // one exchange, and the weights are the B operand of O^T += V^T P^T as they stand.  The tiles are taken from the last one back: the

@@ -475,9 +475,9 @@ __global__ __launch_bounds__(kSumThreads) void prompt_sum_kernel(PromptBwdArgs b
 // ------------------------------------------------------------------ host
 constexpr int kWaves = 4;
 
-// Parts of each 128 keys' queries.  Where the keys' workgroups leave CUs idle, as many as fill the GPU once, with two tiles each or more (16
-// sequences of 54 to 108 rows, 16 on 2 heads of 256: 87 us, whole 132; 1400 rows of 8 heads of 128: 91, in two parts 101, in ten 112).
-// Long ones, eight tiles or more to a part, fill it twice over, as the first keys of a sequence have many times the work of the last ones.
+// Parts of each 128 keys' queries.  Where the keys' workgroups leave CUs idle, as many as fill the GPU once, with two tiles each or more
+// (the whole gradient of 16 sequences of 54 to 108 rows, 16 on 2 heads of 256: 74 us, in one part 157, in ten 95; 1400 rows of 8 heads of
+// 128: 88, in one part 113, in two 97, in ten 109).  Long ones, eight tiles or more to a part, fill it twice over, as the first keys of a sequence have many times the work of the last ones.
 int key_parts(int rows, int n_seq, int n_heads, int n_kv_heads) {
   const long long groups = seq_items<kWaves>(rows, n_seq, 1) * n_kv_heads;
   const long long steps = ((long long)rows / n_seq / kTile + 1) * (n_heads / n_kv_heads);  // of a workgroup, about

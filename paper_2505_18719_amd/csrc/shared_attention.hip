@@ -8,8 +8,8 @@
 // Each leaves its columns' maxima, sums of weights and sums of weighted values, and own ones say which parts there are none of, so
 // that the join has no lengths or groups to look up (its time for 128 environments of 8 groups: 4.8 us, was 6.6).  What bounds it
 // in earnest is a wave's way through a tile, 1.7 us with its SIMD to itself or shared with one (50 environments, 16384 shared
-// tokens, 28 on 4 heads of 128: 38 us, of which ten tiles a workgroup 17, the start 8, the parts' way through memory 5 and their
-// sum 7; unshared 244).
+// tokens, 28 on 4 heads of 128: 36 us, of which ten tiles a workgroup 17, the start 8, the parts' way through memory 5 and their
+// sum 7; unshared 244): scores, maximum, weights and their product with the values follow one another.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
