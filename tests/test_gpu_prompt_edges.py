@@ -44,6 +44,27 @@ def test_queries_of_minus_infinity_give_no_gradient(hd, dtype, H, K, dout):
         assert all(torch.equal(x, bits(y)) for x, y in zip(first, a.back()))
 
 
+@pytest.mark.parametrize("hd,dtype", [(64, BF), (128, FP), (128, BF), (256, BF)])
+@pytest.mark.parametrize("n,most", [(70, 140), (600, 5)])
+def test_queries_of_minus_infinity_among_many_sequences(n, most, hd, dtype):
+    """The same where the keys' workgroups fill the GPU, and where the sequences are more than are listed."""
+    rng = np.random.default_rng(n)
+    lens = rng.integers(1, most + 1, n)
+    a, b = (Case(lens, 8, 4, hd, dtype, seed=n) for _ in range(2))
+    for c in (a, b):
+        c.k[:, :, 3] = c.k[:, :, 3].abs() + 0.1
+    at = rng.choice(np.arange(a.rows)[a.inside], sum(lens) // 5, replace=False)
+    a.q[at, ::2, 3] = -INF
+    a.dout[at, ::2, 7] = NAN
+    b.q[at, ::2] = 0
+    b.dout[at, ::2] = 0
+    a.run()
+    assert (f64(a.out)[at][:, ::2] == 0).all() and np.isneginf(f64(a.lse)[at][:, ::2]).all()
+    a.back()
+    assert (f64(a.dq)[at][:, ::2] == 0).all()
+    against(b, a)
+
+
 @pytest.mark.parametrize("hd,dtype,H,K", KINDS)
 @pytest.mark.parametrize("dout", [None, NAN])
 def test_keys_of_minus_infinity_at_the_start(hd, dtype, H, K, dout):
